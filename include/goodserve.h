@@ -18,6 +18,10 @@
  *   gs_risk_scan     for every active request, the SLO-violation risk test of Sec. 3.4
  *                    (expected finish time under the latest estimates exceeds the SLO) and
  *                    the ascending list of flagged requests (migration candidates).
+ *   gs_expert_route, gs_expert_linear, gs_expert_combine (and their *_backward), gs_clip_grad_norm
+ *                    the operators of the decode-length predictor that feeds pred_decode_len and
+ *                    pred_len to the calls above (Sec. 3.2: a gate over experts, each a small MLP,
+ *                    their answers mixed by the gate's weights), for prediction and for training.
  *   gs_advance_state between the rounds of a stream, folds one round's assignments back
  *                    into the per-instance queue / batch / KV state and carries the smoothed
  *                    queue delay of the EMA step (Algorithm 1) to the next round.
@@ -68,14 +72,16 @@ enum gs_error {
     GS_ERR_CUDA = -3,           /* a CUDA runtime call failed; see gs_last_cuda_error */
     GS_ERR_ALIGN = -4,          /* an array pointer is not 16-byte aligned */
     GS_ERR_NO_DEVICE = -5,      /* no usable CUDA device */
-    GS_ERR_TOO_LARGE = -6       /* gs_risk_scan_noalloc: n_active above GS_NOALLOC_MAX_ACTIVE */
+    GS_ERR_TOO_LARGE = -6,      /* gs_risk_scan_noalloc: n_active above GS_NOALLOC_MAX_ACTIVE */
+    GS_ERR_WORKSPACE = -7       /* gs_expert_linear_backward: workspace smaller than it asked for */
 };
 
 /* bits of the device status word */
 enum gs_dev_status {
     GS_DEV_BAD_INSTANCE = 1,    /* assigned_inst outside [0, n_instances) was clamped */
     GS_DEV_BAD_TYPE = 2,        /* type_id outside [0, n_types) was read as 0 */
-    GS_DEV_BAD_VALUE = 4,       /* negative count or negative/NaN q_ema was read as 0 */
+    GS_DEV_BAD_VALUE = 4,       /* negative count or negative/NaN q_ema was read as 0; NaN score; index of a row or an
+                                   expert outside its range; global gradient norm that is not finite */
     GS_DEV_TIMEOUT = 8,         /* a bounded device-side wait expired (the route kernel's wait for its table
                                    copies); the outputs of that call are invalid */
     GS_DEV_CAND_TRUNCATED = 16, /* more flagged requests than cand_capacity; list was cut */
@@ -161,7 +167,11 @@ enum gs_kernel {
     GS_K_REROUTE = 5,        /* re-routing of the candidates */
     GS_K_EMA = 6,            /* EMA step of directly given coefficients */
     GS_K_SEQUENTIAL = 7,     /* one-request-at-a-time routing */
-    GS_K_COUNT = 8
+    GS_K_EXPERT_ROUTE = 8,   /* length predictor: expert choice, its order, its gradient */
+    GS_K_EXPERT_LINEAR = 9,  /* length predictor: products with the experts' weights, both directions */
+    GS_K_EXPERT_COMBINE = 10,/* length predictor: weighted sums of the experts' rows, both directions */
+    GS_K_CLIP = 11,          /* global gradient norm and clipping */
+    GS_K_COUNT = 12
 };
 
 /* Optional per-kernel timing for benchmarks.  While enabled (on != 0) every kernel launch of
@@ -440,6 +450,166 @@ GS_API int gs_risk_scan_noalloc(const int32_t *assigned_inst, const int32_t *gen
                                 const gs_instances *inst, const gs_types *types,
                                 uint32_t *out_flag_bits, int32_t *out_cand_idx, int64_t cand_capacity,
                                 int64_t *out_cand_count, unsigned *out_status_bits, void *cuda_stream);
+
+/* ---- Operators of the decode-length predictor -----------------------------------------------
+ *
+ * The paper's predictor (Sec. 3.2) is a gate over K experts, each a small MLP; its answer is the
+ * sum of the experts' answers weighted by the gate.  A layer of all experts is one call here:
+ * gs_expert_route turns the gate's logits into choices, weights and an order of rows in which
+ * every expert's rows are consecutive; gs_expert_linear multiplies each row with its expert's
+ * weights; gs_expert_combine adds the rows up again per request.  top_k = n_experts is the
+ * paper's dense mixture.  The same calls with one expert are plain layers (the gate itself).
+ *
+ * Matrices are row-major with a row stride ("ld", in elements).  Their base is 16-byte aligned
+ * and their row stride a multiple of 16 bytes (else GS_ERR_ALIGN); the number of columns may be
+ * odd (columns past it are neither used nor written).  gs_expert_route's logits and
+ * gs_expert_route_backward's d_logits alone may have any row stride.
+ */
+enum gs_dtype { GS_F32 = 0, GS_BF16 = 1, GS_F16 = 2 };
+
+#define GS_MAX_EXPERTS 512
+#define GS_MAX_TOP_K 16
+#define GS_MAX_EXPERT_GROUPS 32
+#define GS_MAX_FEATURES (1 << 20)
+
+enum gs_expert_score { GS_SCORE_SOFTMAX = 0, GS_SCORE_SIGMOID = 1 };
+
+/* How a row of logits x becomes choices and weights, all in float:
+ *   s = softmax(x) or 1 / (1 + exp(-x)) over the row;   c = s + bias  (the choice score)
+ *   with n_groups > 1 (equal, consecutive groups): a group's score is the sum of its group_top
+ *   best c; the top_groups best groups are kept, the others' experts are not chosen;
+ *   the top_k best c are chosen, in descending order (ties everywhere: the lowest index);
+ *   weight = scale * s / (sum of the chosen s + 1e-20) if renormalise, else scale * s. */
+typedef struct gs_expert_router {
+    int32_t n_experts;      /* 1 .. GS_MAX_EXPERTS */
+    int32_t top_k;          /* 1 .. min(GS_MAX_TOP_K, n_experts * top_groups / n_groups) */
+    int32_t score;          /* gs_expert_score */
+    int32_t n_groups;       /* 1 .. GS_MAX_EXPERT_GROUPS, divides n_experts */
+    int32_t top_groups;     /* 1 .. n_groups */
+    int32_t group_top;      /* 1 or 2 */
+    int32_t renormalise;    /* 0 or 1 */
+    float   scale;
+} gs_expert_router;
+
+/*
+ * Routing of n_tokens rows of logits [n_tokens, n_experts] (gs_dtype, row stride ld_logits) to
+ * experts.  bias: float[n_experts], added to the scores for the choice only (balance); may be
+ * NULL.  Outputs:
+ *   out_expert     int32 [n_tokens, top_k]  the chosen experts
+ *   out_weight     float [n_tokens, top_k]
+ *   out_offsets    int32 [n_experts + 1]    expert e's rows are out_offsets[e] .. out_offsets[e+1] - 1
+ *   out_row_token  int32 [n_tokens * top_k] the token of each row; -1 past the last row
+ *   out_token_row  int32 [n_tokens, top_k]  the row of each slot
+ * An expert's rows are in the order of their tokens (a counting sort: the same every time).  The
+ * last three may be NULL together (choices and weights alone).
+ * A logit of -infinity, or a bias of -infinity, takes the expert out of the row's choice; +infinity is read as the largest
+ * finite number; a NaN takes the expert out and sets GS_DEV_BAD_VALUE.  A row with fewer than
+ * top_k experts left has expert -1, weight 0 and row -1 in its last slots (all of them when none is left).
+ * n_tokens * top_k < 2^31.
+ */
+GS_API int gs_expert_route(gs_ctx *ctx, const void *logits, int logits_dtype, int64_t n_tokens, int64_t ld_logits,
+                    const float *bias, const gs_expert_router *router,
+                    int32_t *out_expert, float *out_weight, int32_t *out_offsets, int32_t *out_row_token,
+                    int32_t *out_token_row, void *cuda_stream);
+
+/*
+ * Gradient of gs_expert_route's weights: d_weight float [n_tokens, top_k] to out_d_logits
+ * [n_tokens, n_experts] (the logits' dtype, row stride ld_d_logits), for the choice in `expert`.
+ * The choice itself has no gradient, nor has the bias.  A slot whose expert is -1 contributes
+ * nothing; one outside [-1, n_experts) neither, and sets GS_DEV_BAD_VALUE.
+ */
+GS_API int gs_expert_route_backward(gs_ctx *ctx, const void *logits, int logits_dtype, int64_t n_tokens,
+                    int64_t ld_logits, const gs_expert_router *router, const int32_t *expert,
+                    const float *d_weight, void *out_d_logits, int64_t ld_d_logits, void *cuda_stream);
+
+/* flags of the products and combinations */
+#define GS_EXPERT_RELU 1u        /* gs_expert_linear: out = max(z, 0) */
+#define GS_EXPERT_RELU_INPUT 2u  /* *_backward: the layer below ended in a ReLU; its gradient is zero where its
+                                    output (x, or y of the combination) is not positive */
+
+/*
+ * out[r, :] = act(x[t, :] . W_e^T + bias_e) for the rows r of every expert e, with t = row_token[r],
+ * or t = r when row_token is NULL.
+ *   dtype       GS_BF16 or GS_F16: of x, w and out; sums, bias and activation are in float
+ *   x           [n_x_rows, in_features]       w  [n_experts, out_features, in_features] (rows ld_w apart,
+ *   bias        float [n_experts, out_features] or NULL      experts out_features * ld_w apart)
+ *   offsets     int32 [n_experts + 1] on the device, as gs_expert_route leaves them
+ *   out         [n_rows, out_features]; rows past offsets[n_experts] are not written
+ * Without row_token n_x_rows must be n_rows.  Offsets are clamped into [0, n_rows]; a row_token
+ * outside [0, n_x_rows) is clamped into it and sets GS_DEV_BAD_VALUE.
+ */
+GS_API int gs_expert_linear(gs_ctx *ctx, int dtype, const void *x, int64_t n_x_rows, int64_t ld_x,
+                    const int32_t *row_token, const int32_t *offsets, int32_t n_experts, int64_t n_rows,
+                    const void *w, int64_t ld_w, const float *bias, int32_t in_features, int32_t out_features,
+                    unsigned flags, void *out, int64_t ld_out, void *cuda_stream);
+
+/*
+ * Gradients of gs_expert_linear for dz [n_rows, out_features], the gradient before the activation:
+ *   out_dx[r, :]  = dz[r, :] . W_e                       [n_rows, in_features], the operands' dtype;
+ *                   with GS_EXPERT_RELU_INPUT zero where x[t, :] is not positive.  With row_token it is
+ *                   the gradient per ROW (gs_expert_combine without weights adds a token's rows up)
+ *   out_dw[e]     = sum over e's rows of dz[r, :]^T x[t, :]  float [n_experts, out_features, in_features]
+ *   out_db[e]     = sum over e's rows of dz[r, :]            float [n_experts, out_features]
+ * Each output may be NULL (not all); out_db needs out_dw.  Experts without rows get zeros.  w is
+ * read for out_dx only, x for out_dw and the ReLU.  Sums do not depend on the order of execution.
+ * workspace: device memory of at least gs_expert_linear_backward_workspace bytes, 16-byte aligned
+ * (partial sums where an expert's rows are split; may be NULL when that is 0).
+ */
+GS_API int gs_expert_linear_backward(gs_ctx *ctx, int dtype, const void *dz, int64_t ld_dz,
+                    const void *x, int64_t n_x_rows, int64_t ld_x, const int32_t *row_token,
+                    const int32_t *offsets, int32_t n_experts, int64_t n_rows, const void *w, int64_t ld_w,
+                    int32_t in_features, int32_t out_features, unsigned flags,
+                    void *out_dx, int64_t ld_dx, float *out_dw, int64_t ld_dw, float *out_db,
+                    void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* Bytes of workspace that gs_expert_linear_backward needs for these sizes (0 without out_dw);
+ * negative: a gs_error. */
+GS_API int64_t gs_expert_linear_backward_workspace(const gs_ctx *ctx, int32_t n_experts, int64_t n_rows,
+                    int32_t in_features, int32_t out_features);
+
+/*
+ * out[n, :] = sum over j of weight[n, j] * y[token_row[n, j], :], in float, rounded once to out_dtype
+ * (GS_F32 or y's dtype).  y [n_rows, features] (dtype GS_BF16 or GS_F16); weight float
+ * [n_tokens, top_k], NULL for ones; slots of row -1 are left out (a token with none gets zeros); a
+ * row outside [-1, n_rows) is left out and sets GS_DEV_BAD_VALUE.  The sum is taken in the order of j.
+ */
+GS_API int gs_expert_combine(gs_ctx *ctx, int dtype, const void *y, int64_t n_rows, int64_t ld_y,
+                    const int32_t *token_row, const float *weight, int64_t n_tokens, int32_t top_k,
+                    int32_t features, int out_dtype, void *out, int64_t ld_out, void *cuda_stream);
+
+/*
+ * Gradients of gs_expert_combine for d_out [n_tokens, features] (d_out_dtype GS_F32 or y's dtype):
+ *   out_dy[token_row[n, j], :] = weight[n, j] * d_out[n, :]   (y's dtype; with GS_EXPERT_RELU_INPUT zero
+ *                                where y is not positive); rows that no slot names are not written
+ *   out_d_weight[n, j] = y[token_row[n, j], :] . d_out[n, :]  float; 0 for a slot of row -1.
+ * Either output may be NULL (not both); y is read for out_d_weight and the ReLU only.
+ */
+GS_API int gs_expert_combine_backward(gs_ctx *ctx, int dtype, int d_out_dtype, const void *d_out, int64_t ld_d_out,
+                    const void *y, int64_t n_rows, int64_t ld_y, const int32_t *token_row, const float *weight,
+                    int64_t n_tokens, int32_t top_k, int32_t features, unsigned flags,
+                    void *out_dy, int64_t ld_dy, float *out_d_weight, void *cuda_stream);
+
+/* One gradient of gs_clip_grad_norm: n_elements contiguous elements of `dtype`, aligned to their own
+ * size only (views into one flat buffer are fine).  `out` may be `grad` (in place) or a buffer that
+ * overlaps no other. */
+typedef struct gs_grad {
+    const void *grad;
+    void       *out;
+    int64_t     n_elements;
+    int32_t     dtype;      /* gs_dtype */
+} gs_grad;
+
+/*
+ * Global norm over all tensors, norm = sqrt(sum of squares), and clipping by it:
+ *   out = grad * f,  f = min(1, max_norm / (norm + 1e-6))   computed in float, rounded once.
+ * `grads` is a HOST array (read before the call returns).  Squares and their sum are in double, so
+ * neither the largest nor the smallest gradients are lost, and the sum's order is fixed.
+ * *out_norm: one float on the device.  A norm that is not finite leaves the values as they are
+ * (f = 1) and sets GS_DEV_BAD_VALUE; max_norm >= 0 (not NaN), +infinity never clips.  With `out`
+ * NULL in every entry only the norm is computed.
+ */
+GS_API int gs_clip_grad_norm(gs_ctx *ctx, const gs_grad *grads, int32_t n_tensors, float max_norm,
+                    float *out_norm, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -48,6 +48,15 @@ class _InstanceTable(C.Structure):
                 ("free_kv_tokens", C.c_void_p), ("n_instances", C.c_int32)]
 
 
+class _ExpertRouter(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("n_groups", C.c_int32),
+                ("top_groups", C.c_int32), ("group_top", C.c_int32), ("renormalise", C.c_int32), ("scale", C.c_float)]
+
+
+class _Grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n_elements", C.c_int64), ("dtype", C.c_int32)]
+
+
 class _InstancesMut(C.Structure):
     _fields_ = [("queued_prefill_tokens", C.c_void_p), ("decode_batch", C.c_void_p),
                 ("free_kv_tokens", C.c_void_p), ("q_ema_ms", C.c_void_p),
@@ -102,6 +111,20 @@ def _declare(lib):
     lib.gs_risk_scan_noalloc.argtypes = [vp, vp, vp, vp, vp, i64, C.POINTER(_Instances), C.POINTER(_Types),
                                          vp, vp, i64, vp, vp, vp]
     lib.gs_risk_scan_noalloc.restype = C.c_int
+    lib.gs_expert_route.argtypes = [vp, vp, C.c_int, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.gs_expert_route_backward.argtypes = [vp, vp, C.c_int, i64, i64, vp, vp, vp, vp, i64, vp]
+    lib.gs_expert_linear.argtypes = [vp, C.c_int, vp, i64, i64, vp, vp, i32, i64, vp, i64, vp, i32, i32, u32, vp, i64, vp]
+    lib.gs_expert_linear_backward.argtypes = [vp, C.c_int, vp, i64, vp, i64, i64, vp, vp, i32, i64, vp, i64, i32, i32, u32,
+                                              vp, i64, vp, i64, vp, vp, i64, vp]
+    lib.gs_expert_linear_backward_workspace.argtypes = [vp, i32, i64, i32, i32]
+    lib.gs_expert_linear_backward_workspace.restype = i64
+    lib.gs_expert_combine.argtypes = [vp, C.c_int, vp, i64, i64, vp, vp, i64, i32, i32, C.c_int, vp, i64, vp]
+    lib.gs_expert_combine_backward.argtypes = [vp, C.c_int, C.c_int, vp, i64, vp, i64, i64, vp, vp, i64, i32, i32, u32,
+                                               vp, i64, vp, vp]
+    lib.gs_clip_grad_norm.argtypes = [vp, vp, i32, f32, vp, vp]
+    for name in ("gs_expert_route", "gs_expert_route_backward", "gs_expert_linear", "gs_expert_linear_backward",
+                 "gs_expert_combine", "gs_expert_combine_backward", "gs_clip_grad_norm"):
+        getattr(lib, name).restype = C.c_int
     for name in ("gs_timing_enable", "gs_timing_read", "gs_create", "gs_destroy", "gs_last_cuda_error", "gs_device_status", "gs_route_batch",
                  "gs_route_batch_host", "gs_route_batch_host_deferred", "gs_host_wait", "gs_advance_state", "gs_risk_scan", "gs_risk_scan_host"):
         getattr(lib, name).restype = C.c_int
@@ -159,6 +182,64 @@ def _host_ptr(a, dtype, n: Optional[int], name: str) -> Optional[int]:
     if n is not None and a.size < n:
         raise ValueError(f"{name}: needs {n} elements, has {a.size}")
     return a.ctypes.data
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_OPERANDS = (torch.bfloat16, torch.float16)
+
+
+def _array(t, dtype: torch.dtype, n: int, name: str, device) -> Optional[int]:
+    """A contiguous CUDA tensor of n elements, whatever its shape."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name}: expected a tensor on {device}")
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
+    if t.numel() != n:
+        raise ValueError(f"{name}: needs {n} elements, has {t.numel()}")
+    return t.data_ptr()
+
+
+def _matrix(t, dtype: torch.dtype, rows: int, cols: int, name: str, device):
+    """(address, row stride) of a row-major CUDA matrix; the rows may be further apart than they are wide."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name}: expected a tensor on {device}")
+    if t.dtype is not dtype or t.dim() != 2:
+        raise TypeError(f"{name}: expected a 2-D {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: expected [{rows}, {cols}], got {tuple(t.shape)}")
+    ld, one = t.stride()
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise TypeError(f"{name}: expected rows of consecutive elements, got strides {t.stride()}")
+    return t.data_ptr(), ld if rows > 1 or ld >= cols else (cols + 7) // 8 * 8
+
+
+def _stack(t, dtype: torch.dtype, name: str, device):
+    """(address, row stride) of the experts' matrices [experts, out, in], out rows apart."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise TypeError(f"{name}: expected a tensor on {device}")
+    if t.dtype is not dtype or t.dim() != 3:
+        raise TypeError(f"{name}: expected a 3-D {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
+    (e, o, i), (step, ld, one) = t.shape, t.stride()
+    if o == 1:
+        ld = step if e > 1 else max(ld, (i + 7) // 8 * 8)
+    if (one != 1 and i > 1) or ld < i or (e > 1 and step != o * ld):
+        raise TypeError(f"{name}: expected evenly spaced rows of consecutive elements, got strides {t.stride()}")
+    return t.data_ptr(), ld
+
+
+class ExpertRouter:
+    """How a row of a gate's logits becomes choices and weights (gs_expert_router)."""
+
+    def __init__(self, n_experts: int, top_k: int, score: str = "softmax", n_groups: int = 1, top_groups: int = 1,
+                 group_top: int = 1, renormalise: bool = True, scale: float = 1.0):
+        if score not in ("softmax", "sigmoid"):
+            raise ValueError(f"score: expected 'softmax' or 'sigmoid', got {score!r}")
+        self.n_experts, self.top_k = int(n_experts), int(top_k)
+        self._struct = _ExpertRouter(self.n_experts, self.top_k, 1 if score == "sigmoid" else 0, int(n_groups),
+                                     int(top_groups), int(group_top), 1 if renormalise else 0, float(scale))
+        self._address = C.addressof(self._struct)
 
 
 @dataclass
@@ -434,6 +515,135 @@ class GoodServe:
             _host_ptr(out_cand_idx, np.int32, cap, "out_cand_idx"), cap,
             C.cast(C.byref(count), C.c_void_p), self._stream(stream)))
         return int(count.value)
+
+    # -- the length predictor's operators, same names ---------------------------------------
+    def expert_route(self, logits, router: ExpertRouter, out_expert, out_weight, out_offsets=None, out_row_token=None,
+                     out_token_row=None, bias=None, stream=None):
+        """gs_expert_route.  logits [tokens, experts] (float32, bfloat16 or float16; any row stride);
+        out_expert, out_weight and out_token_row [tokens, top_k], out_offsets [experts + 1],
+        out_row_token [tokens * top_k]; the last three together or not at all."""
+        dev, i32 = self.device, torch.int32
+        code = _DTYPES.get(logits.dtype)
+        if code is None:
+            raise TypeError(f"logits: expected float32, bfloat16 or float16, got {logits.dtype}")
+        n, e, k = logits.shape[0], router.n_experts, router.top_k
+        x, ld = _matrix(logits, logits.dtype, n, e, "logits", dev)
+        self._check(self._lib.gs_expert_route(
+            self._h, x, code, n, ld, _array(bias, torch.float32, e, "bias", dev), router._address,
+            _array(out_expert, i32, n * k, "out_expert", dev), _array(out_weight, torch.float32, n * k, "out_weight", dev),
+            _array(out_offsets, i32, e + 1, "out_offsets", dev), _array(out_row_token, i32, n * k, "out_row_token", dev),
+            _array(out_token_row, i32, n * k, "out_token_row", dev), self._stream(stream)))
+
+    def expert_route_backward(self, logits, router: ExpertRouter, expert, d_weight, out_d_logits, stream=None):
+        """gs_expert_route_backward: d_weight [tokens, top_k] to out_d_logits [tokens, experts]."""
+        dev, n, e, k = self.device, logits.shape[0], router.n_experts, router.top_k
+        code = _DTYPES.get(logits.dtype)
+        if code is None:
+            raise TypeError(f"logits: expected float32, bfloat16 or float16, got {logits.dtype}")
+        x, ld = _matrix(logits, logits.dtype, n, e, "logits", dev)
+        d, ld_d = _matrix(out_d_logits, logits.dtype, n, e, "out_d_logits", dev)
+        self._check(self._lib.gs_expert_route_backward(
+            self._h, x, code, n, ld, router._address, _array(expert, torch.int32, n * k, "expert", dev),
+            _array(d_weight, torch.float32, n * k, "d_weight", dev), d, ld_d, self._stream(stream)))
+
+    def expert_linear(self, x, w, offsets, out, bias=None, row_token=None, relu: bool = False, stream=None):
+        """gs_expert_linear: out[r] = act(x[row_token[r]] . w[e]^T + bias[e]) for the rows r of expert e.
+        w [experts, out, in]; without row_token x has a row for every row of out."""
+        dev, dt = self.device, x.dtype
+        if dt not in _OPERANDS:
+            raise TypeError(f"x: expected bfloat16 or float16, got {dt}")
+        wp, ldw = _stack(w, dt, "w", dev)
+        e, o, i = w.shape
+        rows, nx = out.shape[0], x.shape[0]
+        xp, ldx = _matrix(x, dt, nx, i, "x", dev)
+        yp, ldy = _matrix(out, dt, rows, o, "out", dev)
+        self._check(self._lib.gs_expert_linear(
+            self._h, _DTYPES[dt], xp, nx, ldx, _array(row_token, torch.int32, rows, "row_token", dev),
+            _array(offsets, torch.int32, e + 1, "offsets", dev), e, rows, wp, ldw,
+            _array(bias, torch.float32, e * o, "bias", dev), i, o, 1 if relu else 0, yp, ldy, self._stream(stream)))
+
+    def expert_linear_backward(self, dz, x, w, offsets, dx=None, dw=None, db=None, row_token=None,
+                               relu_input: bool = False, stream=None):
+        """gs_expert_linear_backward: fills those of dx [rows, in], dw [experts, out, in] (float32) and
+        db [experts, out] (float32) that are given.  The partial sums' workspace comes from PyTorch's
+        allocator, on the stream of the call."""
+        dev, dt = self.device, dz.dtype
+        if dt not in _OPERANDS:
+            raise TypeError(f"dz: expected bfloat16 or float16, got {dt}")
+        wp, ldw = _stack(w, dt, "w", dev)
+        e, o, i = w.shape
+        rows, nx = dz.shape[0], x.shape[0]
+        zp, ldz = _matrix(dz, dt, rows, o, "dz", dev)
+        xp, ldx = _matrix(x, dt, nx, i, "x", dev)
+        dxp = dwp = workspace = None
+        lddx = lddw = need = 0
+        if dx is not None:
+            dxp, lddx = _matrix(dx, dt, rows, i, "dx", dev)
+        if dw is not None:
+            if dw.shape != w.shape:
+                raise ValueError(f"dw: expected {tuple(w.shape)}, got {tuple(dw.shape)}")
+            dwp, lddw = _stack(dw, torch.float32, "dw", dev)
+            need = self._lib.gs_expert_linear_backward_workspace(self._h, e, rows, i, o)
+            if need > 0:
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+                if stream is not None:
+                    workspace.record_stream(stream)
+        self._check(self._lib.gs_expert_linear_backward(
+            self._h, _DTYPES[dt], zp, ldz, xp, nx, ldx, _array(row_token, torch.int32, rows, "row_token", dev),
+            _array(offsets, torch.int32, e + 1, "offsets", dev), e, rows, wp, ldw, i, o, 2 if relu_input else 0,
+            dxp, lddx, dwp, lddw, _array(db, torch.float32, e * o, "db", dev),
+            None if workspace is None else workspace.data_ptr(), max(need, 0), self._stream(stream)))
+
+    def expert_combine(self, y, token_row, out, weight=None, stream=None):
+        """gs_expert_combine: out[n] = sum over j of weight[n, j] * y[token_row[n, j]]; out in y's dtype or float32."""
+        dev, dt = self.device, y.dtype
+        if dt not in _OPERANDS:
+            raise TypeError(f"y: expected bfloat16 or float16, got {dt}")
+        if out.dtype is not dt and out.dtype is not torch.float32:
+            raise TypeError(f"out: expected {dt} or float32, got {out.dtype}")
+        (n, k), (rows, f) = token_row.shape, y.shape
+        yp, ldy = _matrix(y, dt, rows, f, "y", dev)
+        op, ldo = _matrix(out, out.dtype, n, f, "out", dev)
+        self._check(self._lib.gs_expert_combine(
+            self._h, _DTYPES[dt], yp, rows, ldy, _array(token_row, torch.int32, n * k, "token_row", dev),
+            _array(weight, torch.float32, n * k, "weight", dev), n, k, f, _DTYPES[out.dtype], op, ldo, self._stream(stream)))
+
+    def expert_combine_backward(self, d_out, y, token_row, dy=None, weight=None, d_weight=None, relu: bool = False,
+                                stream=None):
+        """gs_expert_combine_backward: fills those of dy [rows, features] and d_weight [tokens, top_k] that are given."""
+        dev, dt = self.device, y.dtype
+        if dt not in _OPERANDS:
+            raise TypeError(f"y: expected bfloat16 or float16, got {dt}")
+        if d_out.dtype is not dt and d_out.dtype is not torch.float32:
+            raise TypeError(f"d_out: expected {dt} or float32, got {d_out.dtype}")
+        (n, k), (rows, f) = token_row.shape, y.shape
+        yp, ldy = _matrix(y, dt, rows, f, "y", dev)
+        gp, ldg = _matrix(d_out, d_out.dtype, n, f, "d_out", dev)
+        dyp, lddy = (None, 0) if dy is None else _matrix(dy, dt, rows, f, "dy", dev)
+        self._check(self._lib.gs_expert_combine_backward(
+            self._h, _DTYPES[dt], _DTYPES[d_out.dtype], gp, ldg, yp, rows, ldy,
+            _array(token_row, torch.int32, n * k, "token_row", dev), _array(weight, torch.float32, n * k, "weight", dev),
+            n, k, f, 2 if relu else 0, dyp, lddy, _array(d_weight, torch.float32, n * k, "d_weight", dev), self._stream(stream)))
+
+    def clip_grad_norm(self, grads, max_norm: float, out_norm, outs=None, write: bool = True, stream=None):
+        """gs_clip_grad_norm over contiguous tensors (float32, bfloat16 or float16): scales them in place, or into
+        ``outs``, so that their global norm is at most max_norm.  out_norm: one float32 on the device.  With
+        ``write=False`` only the norm is computed."""
+        if outs is not None and len(outs) != len(grads):
+            raise ValueError(f"outs: needs {len(grads)} tensors, has {len(outs)}")
+        table, dev = (_Grad * len(grads))(), self.device
+        for k, g in enumerate(grads):
+            code = _DTYPES.get(g.dtype)
+            if code is None or g.device != dev or not g.is_contiguous():
+                raise TypeError(f"grads[{k}]: expected a contiguous float32, bfloat16 or float16 tensor on {dev}")
+            o = g
+            if outs is not None:
+                o = outs[k]
+                if o.dtype is not g.dtype or o.device != dev or not o.is_contiguous() or o.numel() != g.numel():
+                    raise TypeError(f"outs[{k}]: expected a contiguous {g.dtype} tensor of {g.numel()} elements on {dev}")
+            table[k] = (g.data_ptr(), o.data_ptr() if write else None, g.numel(), code)
+        self._check(self._lib.gs_clip_grad_norm(self._h, C.addressof(table), len(grads), float(max_norm),
+                                                _array(out_norm, torch.float32, 1, "out_norm", dev), self._stream(stream)))
 
     def device_status(self, stream=None) -> int:
         bits = C.c_uint(0)

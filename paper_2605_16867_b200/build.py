@@ -13,7 +13,8 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libgoodserve.so")
 COUNT_LIB_PATH = os.path.join(_PKG, "libgoodserve_count.so")    # the measuring build (-DGS_COUNT_EVALS)
 DEBUG_LIB_PATH = os.path.join(_PKG, "libgoodserve_debug.so")    # the checking build (-DGS_DEBUG)
-SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu")
+SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu", "operators_api.cu", "experts_route.cu",
+           "experts_linear.cu", "experts_combine.cu", "clip.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--shared",
               "-cudart", "shared")

@@ -4,27 +4,14 @@
 #include <string.h>
 
 #include "gs_internal.cuh"
+#include "api_util.cuh"
+#include "operators.cuh"
+
+using gs::cuda_fail;
+using gs::DeviceGuard;
+using gs::misaligned;
 
 namespace {
-
-inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-int cuda_fail(gs_ctx *ctx, cudaError_t e) {
-    if (ctx) ctx->last_cuda_error = (int)e;
-    return GS_ERR_CUDA;
-}
-
-// Makes the context's device current for the duration of a call.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-        if (prev == dev) prev = -1;
-    }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
 
 int check_pool(const gs_ctx *ctx, const gs_instances *inst, const gs_types *types, bool device_ptrs) {
     if (!ctx || !inst || !types) return GS_ERR_INVALID_ARG;
@@ -126,6 +113,7 @@ GS_API const char *gs_strerror(int code) {
         case GS_ERR_CUDA: return "a CUDA runtime call failed (see gs_last_cuda_error)";
         case GS_ERR_ALIGN: return "array pointer is not 16-byte aligned";
         case GS_ERR_NO_DEVICE: return "no usable CUDA device";
+        case GS_ERR_WORKSPACE: return "workspace smaller than gs_expert_linear_backward_workspace asks for";
         case GS_ERR_TOO_LARGE: return "n_active exceeds GS_NOALLOC_MAX_ACTIVE, the fixed scratch of the no-allocation scan";
         default: return "unknown error code";
     }
@@ -142,7 +130,7 @@ GS_API int gs_create(gs_ctx **out, int device, int max_instances, int max_types)
     DeviceGuard guard(device);
     if (!guard.ok) return GS_ERR_NO_DEVICE;
 
-    gs_ctx *ctx = new (std::nothrow) gs_ctx();
+    gs::Context *ctx = new (std::nothrow) gs::Context();
     if (!ctx) return GS_ERR_INVALID_ARG;
     memset(ctx, 0, sizeof(*ctx));
     ctx->device = device;
@@ -175,13 +163,16 @@ GS_API int gs_create(gs_ctx **out, int device, int max_instances, int max_types)
         {(void **)&s.deltas, 3 * Mx * sizeof(unsigned long long)},
         {(void **)&s.scan_counts, gs::kMaxScanCtas * sizeof(unsigned)},
         {(void **)&s.status, 256},
+        {(void **)&ctx->ops.expert_counts, gs::kExpertCountBytes},
+        {(void **)&ctx->ops.clip_partials, gs::kMaxClipCtas * sizeof(double)},
     };
     for (auto &a : allocs) {
         e = cudaMalloc(a.p, a.bytes);
         if (e == cudaSuccess) e = cudaMemset(*a.p, 0, a.bytes);
         if (e != cudaSuccess) { gs_destroy(ctx); return GS_ERR_CUDA; }
     }
-    if (gs::configure_route(ctx) != cudaSuccess || gs::configure_prologue() != cudaSuccess) {
+    if (gs::configure_route(ctx) != cudaSuccess || gs::configure_prologue() != cudaSuccess ||
+        gs::configure_expert_linear() != cudaSuccess) {
         gs_destroy(ctx);
         return GS_ERR_CUDA;
     }
@@ -193,7 +184,8 @@ GS_API int gs_destroy(gs_ctx *ctx) {
     if (!ctx) return GS_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->device);
     gs::Scratch &s = ctx->s;
-    void *ptrs[] = {s.rows, s.row_bounds, s.group_bounds, s.row_p, s.start_table, s.headers, s.table_info, s.cand_table, s.pool, s.bucket_list, s.start_list, s.chord, s.q_by_g, s.deltas, s.scan_counts, s.status, ctx->stage, ctx->scan_stage};
+    void *ptrs[] = {s.rows, s.row_bounds, s.group_bounds, s.row_p, s.start_table, s.headers, s.table_info, s.cand_table, s.pool, s.bucket_list, s.start_list, s.chord, s.q_by_g, s.deltas, s.scan_counts, s.status, ctx->stage, ctx->scan_stage,
+                    gs::operator_scratch(ctx).expert_counts, gs::operator_scratch(ctx).clip_partials};
     for (void *p : ptrs) if (p) cudaFree(p);
     if (ctx->pending) for (auto &t : *ctx->pending) { cudaEventDestroy(t.start); cudaEventDestroy(t.stop); }
     if (ctx->free_events) for (cudaEvent_t ev : *ctx->free_events) cudaEventDestroy(ev);
@@ -205,7 +197,7 @@ GS_API int gs_destroy(gs_ctx *ctx) {
     }
     delete ctx->pending;
     delete ctx->free_events;
-    delete ctx;
+    delete static_cast<gs::Context *>(ctx);
     return GS_OK;
 }
 

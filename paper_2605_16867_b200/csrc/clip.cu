@@ -1,0 +1,152 @@
+// Global gradient norm over many tensors, and clipping by it.
+//   norm = sqrt(sum g^2);   out = g * min(1, max_norm / (norm + 1e-6))
+// Bound by memory: one read of everything for the norm, one read and one write for the clipping
+// (the read comes from L2 as far as the gradients fit).  Squares and sums are in double (a float's
+// square leaves the range of a float from 1.8e19 up and 1e-23 down); every CTA leaves one partial
+// sum, which the next launch adds in a fixed order, so the norm is the same every time.
+#include "operators.cuh"
+
+namespace gs {
+namespace {
+
+constexpr int kClipThreads = 512;
+constexpr int kClipTensors = 256;                    // tensors of one launch (their table travels as a kernel argument)
+constexpr int kClipChunk = 16384;                    // elements that a CTA takes at a time
+
+struct ClipTable {
+    int n;
+    int chunk_start[kClipTensors + 1];               // chunks before each tensor
+    const void *grad[kClipTensors];
+    void *out[kClipTensors];
+    int64_t n_elements[kClipTensors];
+    unsigned char dtype[kClipTensors];
+};
+
+__device__ __forceinline__ int tensor_of(const ClipTable &t, int chunk) {
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.chunk_start[mid] <= chunk) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n; i += kClipThreads) { const double v = (double)to_float(g[i]); sum = fma(v, v, sum); }
+    return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const T *g, T *out, int n, float f) {
+    for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(to_float(g[i]) * f);
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double part[kClipThreads / 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double sum = 0.0;
+    for (int w = 0; w < kClipThreads / 32; ++w) sum += part[w];
+    __syncthreads();
+    return sum;
+}
+
+__global__ void __launch_bounds__(kClipThreads)
+norm_kernel(const __grid_constant__ ClipTable t, double *__restrict__ partials)
+{
+    dependent_begin();
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < t.chunk_start[t.n]; c += gridDim.x) {
+        const int k = tensor_of(t, c);
+        const int64_t first = (int64_t)(c - t.chunk_start[k]) * kClipChunk;
+        const int n = (int)min((int64_t)kClipChunk, t.n_elements[k] - first);
+        if (t.dtype[k] == GS_F32) sum += chunk_square((const float *)t.grad[k] + first, n);
+        else if (t.dtype[k] == GS_BF16) sum += chunk_square((const __nv_bfloat16 *)t.grad[k] + first, n);
+        else sum += chunk_square((const __half *)t.grad[k] + first, n);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) partials[blockIdx.x] = sum;
+}
+
+// The factor, from all partial sums (every CTA adds them in the same order).
+__device__ __forceinline__ float clip_factor(const double *__restrict__ partials, int n_partials, float max_norm,
+                                             float *out_norm, unsigned *status) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n_partials; i += kClipThreads) sum += partials[i];
+    const float norm = (float)sqrt(block_sum(sum));
+    const bool finite = norm <= 3.402823466e38f;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && out_norm) {
+        *out_norm = norm;
+        if (!finite) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    }
+    return finite ? fminf(1.f, max_norm / (norm + 1e-6f)) : 1.f;
+}
+
+__global__ void __launch_bounds__(kClipThreads)
+clip_kernel(const __grid_constant__ ClipTable t, const double *__restrict__ partials, int n_partials, float max_norm,
+            float *__restrict__ out_norm, unsigned *__restrict__ status)
+{
+    dependent_begin();
+    const float f = clip_factor(partials, n_partials, max_norm, out_norm, status);
+    for (int c = blockIdx.x; c < t.chunk_start[t.n]; c += gridDim.x) {
+        const int k = tensor_of(t, c);
+        const int64_t first = (int64_t)(c - t.chunk_start[k]) * kClipChunk;
+        const int n = (int)min((int64_t)kClipChunk, t.n_elements[k] - first);
+        if (t.dtype[k] == GS_F32) chunk_scale((const float *)t.grad[k] + first, (float *)t.out[k] + first, n, f);
+        else if (t.dtype[k] == GS_BF16) chunk_scale((const __nv_bfloat16 *)t.grad[k] + first, (__nv_bfloat16 *)t.out[k] + first, n, f);
+        else chunk_scale((const __half *)t.grad[k] + first, (__half *)t.out[k] + first, n, f);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_clip(gs_ctx *ctx, const gs_grad *grads, int n_tensors, float max_norm, bool write,
+                        float *out_norm, cudaStream_t st)
+{
+    // pass 0: partial sums of every table; pass 1: the factor and the values
+    double *partials = operator_scratch(ctx).clip_partials;
+    int n_tables = (n_tensors + kClipTensors - 1) / kClipTensors;
+    if (n_tables < 1) n_tables = 1;
+    int per_table = kMaxClipCtas / n_tables;
+    if (per_table > ctx->n_sm * 4) per_table = ctx->n_sm * 4;
+    if (per_table < 1) return cudaErrorInvalidValue;
+    int n_partials = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int first = 0, table = 0; table < n_tables; first += kClipTensors, ++table) {
+            if (pass == 1 && !write && table > 0) break;
+            ClipTable t;
+            t.n = 0;
+            t.chunk_start[0] = 0;
+            int64_t chunks = 0;
+            for (int i = first; i < n_tensors && i < first + kClipTensors; ++i) {
+                if (grads[i].n_elements == 0) continue;
+                t.grad[t.n] = grads[i].grad;
+                t.out[t.n] = grads[i].out;
+                t.n_elements[t.n] = grads[i].n_elements;
+                t.dtype[t.n] = (unsigned char)grads[i].dtype;
+                chunks += (grads[i].n_elements + kClipChunk - 1) / kClipChunk;
+                if (chunks > INT32_MAX) return cudaErrorInvalidValue;
+                t.chunk_start[++t.n] = (int)chunks;
+            }
+            if (pass == 1 && !write) { t.n = 0; chunks = 0; }
+            const int ctas = chunks < 1 ? 1 : chunks < per_table ? (int)chunks : per_table;
+            LaunchTimer timer(ctx, GS_K_CLIP, st);
+            cudaError_t e;
+            if (pass == 0) {
+                e = launch_dependent(norm_kernel, dim3(ctas), dim3(kClipThreads), 0, st, t, partials + n_partials);
+                n_partials += ctas;
+            } else {
+                e = launch_dependent(clip_kernel, dim3(ctas), dim3(kClipThreads), 0, st, t, (const double *)partials,
+                                     n_partials, max_norm, table == 0 ? out_norm : nullptr, ctx->s.status);
+            }
+            if (e != cudaSuccess) return e;
+        }
+    }
+    return cudaSuccess;
+}
+
+}  // namespace gs
