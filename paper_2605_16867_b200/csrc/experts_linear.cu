@@ -1,175 +1,832 @@
-// Products with the experts' weights:
+// Products with the experts' weights, on the tensor cores:
 //   forward   y[r]  = act(x[t(r)] W_e^T + b_e)         per row r of expert e
 //   backward  dx[r] = dz[r] W_e  (zero where x[t(r)] <= 0),   dW_e = sum_r dz[r]^T x[t(r)],   db_e = sum_r dz[r]
-// Plain tiles: 64 x 64 results per CTA, sixteen of the contraction at a time through shared memory.
+//
+// Every kernel is persistent: one pair of CTAs per pair of SMs takes tiles in turn.  Six or seven
+// warps have fixed parts: warp 0 copies operand tiles into a ring of shared-memory stages, warp 1 of
+// the leader issues the matrix instructions, warps 2-5 move finished sums from tensor memory to
+// global memory while the next tile is already being summed (two sets of sums in tensor memory).
+// Which rows belong to which expert is read from the offsets on the device; the host knows only
+// their number.
+//
+// In y and dx the tile's 256 "M" rows are weights (features of the result), its "N" columns are
+// requests: few rows per expert then cost little (N can be small, the weights are read once), and
+// with many rows a pair reads 64 KB per 64 of the contraction for 256 x 256 results.
+#include <type_traits>
+
 #include "operators.cuh"
+#include "tensor_core.cuh"
 
 namespace gs {
 namespace {
 
-constexpr int kTile = 64, kDepth = 16, kThreads = 256;
+using namespace tc;
 
-// Tile t of all experts' row tiles: its expert and its rows; false past the last.
-__device__ __forceinline__ bool row_tile(const int32_t *__restrict__ offsets, int n_experts, int n_rows, int t,
-                                         int *expert, int2 *rows) {
-    for (int e = 0; e < n_experts; ++e) {
-        const int2 r = expert_rows(offsets, e, n_rows);
-        const int tiles = (r.y - r.x + kTile - 1) / kTile;
-        if (t < tiles) { *expert = e; *rows = make_int2(r.x + t * kTile, min(r.x + (t + 1) * kTile, r.y)); return true; }
-        t -= tiles;
+constexpr int kDepth = 64;                      // of the contraction per stage: one 128-byte row of 16-bit values
+constexpr int kHalfM = 128;                     // rows of the result per CTA of a pair
+constexpr int kTileM = 2 * kHalfM;
+constexpr uint32_t kABytes = kHalfM * 128;
+constexpr int kWarpProducer = 0, kWarpMma = 1;      // the next four (eight in dW) store, dW's last one clears
+constexpr int kMaxStages = 10;
+
+struct Barriers {
+    uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], sums_full[2], sums_empty[2];
+    uint32_t tmem;
+    int failed;
+};
+
+template <typename T> constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+
+__device__ __forceinline__ void setup_pair(Barriers *b, int stages, int store_warps, int warp, int lane) {
+    if (warp == 0 && lane == 0) {
+        for (int s = 0; s < stages; ++s) {
+            bar_init(smem_u32(&b->full[s]), 2);                 // one from each CTA, and its copies' bytes
+            bar_init(smem_u32(&b->empty[s]), 1);
+            bar_init(smem_u32(&b->landed[s]), 1);
+        }
+        for (int i = 0; i < 2; ++i) { bar_init(smem_u32(&b->sums_full[i]), 1); bar_init(smem_u32(&b->sums_empty[i]), 2 * store_warps); }
+        b->failed = 0;
+        bar_init_done();
     }
-    return false;
 }
 
-// kBackward: out = dz W_e (contraction over w's rows); else out = x W_e^T
-template <typename T, bool kBackward>
-__global__ void __launch_bounds__(kThreads)
-rows_kernel(const T *__restrict__ a, int64_t ld_a, const int32_t *__restrict__ a_row, int n_a_rows,
-            const int32_t *__restrict__ offsets, int n_experts, int n_rows, const T *__restrict__ w, int64_t ld_w,
-            int w_rows, int depth, int cols, const float *__restrict__ bias, bool relu,
-            const T *__restrict__ mask, int64_t ld_mask, const int32_t *__restrict__ mask_row, int n_mask_rows,
-            T *__restrict__ out, int64_t ld_out, unsigned *__restrict__ status)
-{
-    __shared__ float sa[kDepth][kTile + 1], sw[kDepth][kTile + 1];
-    dependent_begin();
-    int e;
-    int2 rows;
-    if (!row_tile(offsets, n_experts, n_rows, blockIdx.x, &e, &rows)) return;
-    const int col0 = blockIdx.y * kTile;
-    const T *we = w + (int64_t)e * w_rows * ld_w;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[4][4] = {};
-    bool bad = false;
-    for (int k0 = 0; k0 < depth; k0 += kDepth) {
-        for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-            const int r = i / kDepth, k = k0 + i % kDepth;
-            float v = 0.f;
-            if (rows.x + r < rows.y && k < depth) {
-                int src = rows.x + r;
-                if (a_row) {
-                    src = a_row[src];
-                    if (src < 0 || src >= n_a_rows) { bad = true; src = min(max(src, 0), n_a_rows - 1); }
-                }
-                v = to_float(a[src * ld_a + k]);
-            }
-            sa[i % kDepth][r] = v;
-            const int c = col0 + r;
-            sw[i % kDepth][r] = c < cols && k < depth ? to_float(kBackward ? we[k * ld_w + c] : we[c * ld_w + k]) : 0.f;
-        }
-        __syncthreads();
+// Position in the ring of stages: stage and the parity of its current round.
+struct Ring {
+    int stage = 0, round = 0;
+    __device__ __forceinline__ void next(int stages) { if (++stage == stages) { stage = 0; round ^= 1; } }
+};
+
+// Rows of expert e = base + lane, for the lanes of one warp (all experts in turn).  Offsets may be
+// anything: they are clamped into [0, n_rows] and made ascending, so that no two experts share a
+// row; `before` carries the end of the last expert.
+__device__ __forceinline__ int2 ascending_rows(const int32_t *__restrict__ offsets, int e, int n_experts, int n_rows, int lane, int *before) {
+    int a = e < n_experts ? min(max(offsets[e], 0), n_rows) : 0, b = e < n_experts ? min(max(offsets[e + 1], 0), n_rows) : 0;
+    a = max(a, *before);
+    b = max(a, b);
+    int most = b;
 #pragma unroll
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty * 4 + i], sw[k][tx * 4 + j], acc[i][j]);
-        __syncthreads();
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(kFull, most, o);
+        if (lane >= o) most = max(most, up);
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int r = rows.x + ty * 4 + i, c = col0 + tx * 4 + j;
-            if (r >= rows.y || c >= cols) continue;
-            float v = acc[i][j];
-            if (bias) v += bias[(int64_t)e * cols + c];
-            if (relu) v = v > 0.f || v != v ? v : 0.f;
-            if (mask) {
-                const int m = mask_row ? min(max(mask_row[r], 0), n_mask_rows - 1) : r;
-                if (!(to_float(mask[m * ld_mask + c]) > 0.f)) v = 0.f;
-            }
-            out[r * ld_out + c] = from_float<T>(v);
-        }
-    if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    const int up = __shfl_up_sync(kFull, most, 1);
+    if (lane > 0) a = max(a, up);
+    *before = __shfl_sync(kFull, most, 31);
+    return make_int2(a, max(a, b));
 }
 
-// One expert's dW tile; the first column tile also leaves db.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-weights_kernel(const T *__restrict__ dz, int64_t ld_dz, const T *__restrict__ x, int64_t ld_x,
-               const int32_t *__restrict__ x_row, int n_x_rows, const int32_t *__restrict__ offsets, int n_rows,
-               int n_out, int n_in, float *__restrict__ dw, int64_t ld_dw, float *__restrict__ db, unsigned *__restrict__ status)
-{
-    __shared__ float sa[kDepth][kTile + 1], sw[kDepth][kTile + 1];
-    dependent_begin();
-    const int e = blockIdx.z, out0 = blockIdx.y * kTile, in0 = blockIdx.x * kTile;
-    const int2 rows = expert_rows(offsets, e, n_rows);
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    // (two levels of sums: one float that takes tens of thousands of terms in turn loses several bits)
-    float acc[4][4] = {}, bias[4] = {}, acc2[4][4] = {}, bias2[4] = {};
-    bool bad = false;
-    for (int r0 = rows.x; r0 < rows.y; r0 += kDepth) {
-        for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-            const int r = r0 + i / kTile, c = i % kTile;
-            float v = 0.f, u = 0.f;
-            if (r < rows.y) {
-                if (out0 + c < n_out) v = to_float(dz[r * ld_dz + out0 + c]);
-                int src = r;
-                if (x_row) {
-                    src = x_row[src];
-                    if (src < 0 || src >= n_x_rows) { bad = true; src = min(max(src, 0), n_x_rows - 1); }
-                }
-                if (in0 + c < n_in) u = to_float(x[src * ld_x + in0 + c]);
-            }
-            sa[i / kTile][c] = v;
-            sw[i / kTile][c] = u;
+// Where the rows of expert e begin and end, and the tiles of all experts before it.
+__device__ __forceinline__ void scan_row_tiles(const int32_t *__restrict__ offsets, int n_experts, int n_rows, int rows_per_tile,
+                                               int *tile_start, int *row_start, int *row_end, int lane) {
+    int before = 0, end = 0;
+    for (int base = 0; base < n_experts; base += 32) {
+        const int e = base + lane;
+        const int2 r = ascending_rows(offsets, e, n_experts, n_rows, lane, &end);
+        const int own = (r.y - r.x + rows_per_tile - 1) / rows_per_tile;
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(kFull, sum, o);
+            if (lane >= o) sum += up;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = sa[k][ty * 4 + i];
-                bias[i] += v;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(v, sw[k][tx * 4 + j], acc[i][j]);
-            }
-        __syncthreads();
-        if ((r0 - rows.x) % 512 == 512 - kDepth || r0 + kDepth >= rows.y)
-            for (int i = 0; i < 4; ++i) {
-                bias2[i] += bias[i];
-                bias[i] = 0.f;
-                for (int j = 0; j < 4; ++j) { acc2[i][j] += acc[i][j]; acc[i][j] = 0.f; }
-            }
+        if (e < n_experts) { tile_start[e] = before + sum - own; row_start[e] = r.x; row_end[e] = r.y; }
+        before += __shfl_sync(kFull, sum, 31);
     }
-    for (int i = 0; i < 4; ++i) {
-        const int o = out0 + ty * 4 + i;
-        if (o >= n_out) continue;
-        if (db && in0 == 0 && tx == 0) db[(int64_t)e * n_out + o] = bias2[i];
-        for (int j = 0; j < 4; ++j)
-            if (in0 + tx * 4 + j < n_in) dw[((int64_t)e * n_out + o) * ld_dw + in0 + tx * 4 + j] = acc2[i][j];
+    if (lane == 0) tile_start[n_experts] = before;
+}
+
+// A token index, held inside the matrix it points into.
+__device__ __forceinline__ int safe_token(int t, int n, bool *bad) {
+    if ((unsigned)t < (unsigned)n) return t;
+    *bad = true;
+    return min(max(t, 0), n - 1);
+}
+
+// ---- y and dx ---------------------------------------------------------------------------------
+
+struct RowsArgs {
+    const int32_t *offsets, *row_token;         // row_token: rows of the N operand (forward) or of the mask (backward)
+    int n_experts, n_rows, n_tokens;            // n_tokens: rows that row_token points into
+    int features, depth;                        // of the result; of the contraction
+    const float *bias;
+    bool relu;
+    const void *mask;
+    int64_t ld_mask;
+    void *out;
+    int64_t ld_out;
+    unsigned *status;
+};
+
+template <int kN> struct RowsShape {
+    static constexpr uint32_t kBBytes = kN / 2 * 128;
+    static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kN == 256 ? 6 : kN == 128 ? 8 : kN == 64 ? 9 : 10;
+    static constexpr int kStoreBytes = 4 * 2048;             // per warp: 32 requests x 32 features
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + sizeof(Barriers) + (3 * GS_MAX_EXPERTS + 4) * sizeof(int);
+    static constexpr int kTmem = 2 * kN < 32 ? 32 : 2 * kN;
+};
+
+// kDx: the weights' tile has its features contiguous (the contraction runs over their rows).
+template <typename T, bool kDx, int kN, bool kGather>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1)
+rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const RowsArgs p)
+{
+    using S = RowsShape<kN>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    unsigned char *store = smem + S::kStages * S::kStageBytes;
+    Barriers *bars = reinterpret_cast<Barriers *>(store + S::kStoreBytes);
+    int *tile_start = reinterpret_cast<int *>(bars + 1), *row_start = tile_start + GS_MAX_EXPERTS + 1, *row_end = row_start + GS_MAX_EXPERTS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    volatile int *failed = &bars->failed;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    setup_pair(bars, S::kStages, 4, warp, lane);
+    if (warp == kWarpMma) tmem_alloc<S::kTmem>(smem_u32(&bars->tmem));
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0) scan_row_tiles(p.offsets, p.n_experts, p.n_rows, kN, tile_start, row_start, row_end, lane);
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+
+    const uint32_t tmem = bars->tmem;
+    const int m_tiles = (p.features + kTileM - 1) / kTileM, k_steps = (p.depth + kDepth - 1) / kDepth;
+    const int64_t n_tiles = (int64_t)tile_start[p.n_experts] * m_tiles;
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+    if (warp == kWarpProducer) {
+        if (lane == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
+        Ring ring;
+        int e = 0;
+        bool bad = false, ok = true;
+        for (int64_t t = pair; t < n_tiles && ok; t += n_pairs) {
+            const int rt = (int)(t / m_tiles), m0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM;
+            while (tile_start[e + 1] <= rt) ++e;
+            const int r0 = row_start[e] + (rt - tile_start[e]) * kN + (int)rank * (kN / 2);
+            constexpr int kGroups = (kN / 2 + 127) / 128;      // of four rows per lane
+            int token[kGroups][4];
+            if (kGather) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = min(r0 + (g * 32 + lane) * 4 + i, row_end[e] - 1);
+                        token[g][i] = safe_token(p.row_token[r], p.n_tokens, &bad);
+                    }
+            }
+            for (int k = 0; k < k_steps; ++k) {
+                if (!warp_wait(smem_u32(&bars->empty[ring.stage]), ring.round ^ 1, failed)) { ok = false; break; }
+                const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes), b = a + kABytes;
+                const uint32_t full = in_leader(smem_u32(&bars->full[ring.stage]));
+                if (lane == 0) {
+                    bar_expect(full, S::kStageBytes);
+                    if (kDx) {
+                        copy_3d(&map_w, a, full, m0, k * kDepth, e);
+                        copy_3d(&map_w, a + kABytes / 2, full, m0 + 64, k * kDepth, e);
+                    } else {
+                        copy_3d(&map_w, a, full, k * kDepth, m0, e);
+                    }
+                    if (!kGather) copy_2d(&map_x, b, full, k * kDepth, r0);
+                }
+                if (kGather) {
+                    __syncwarp();
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g) {
+                        const int row = (g * 32 + lane) * 4;
+                        if (row < kN / 2)
+                            copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[g][0], token[g][1], token[g][2], token[g][3]);
+                    }
+                }
+                ring.next(S::kStages);
+            }
+        }
+        if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
+    } else if (warp == kWarpMma) {
+        if (rank == 0 && lane == 0) {
+            constexpr uint32_t kInstr = instruction(kBf16<T>, kDx, false, kTileM, kN);
+            Ring ring;
+            int use = 0;
+            bool ok = true;
+            for (int64_t t = pair; t < n_tiles && ok; t += n_pairs, ++use) {
+                const uint32_t sums = tmem + (use & 1) * kN;
+                if (!bar_wait(smem_u32(&bars->sums_empty[use & 1]), ((use >> 1) & 1) ^ 1, failed)) break;
+                fence_after();
+                for (int k = 0; k < k_steps; ++k) {
+                    if (!bar_wait(smem_u32(&bars->full[ring.stage]), ring.round, failed)) { ok = false; break; }
+                    fence_after();
+                    const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes);
+                    const uint64_t da = operand(a, kDx ? kABytes / 2 : 16), db = operand(a + kABytes, 16);
+#pragma unroll
+                    for (int i = 0; i < kDepth / 16; ++i)
+                        mma(sums, da + (kDx ? i * 2048 : i * 32) / 16, db + i * 32 / 16, kInstr, k + i > 0);
+                    commit(smem_u32(&bars->empty[ring.stage]));
+                    ring.next(S::kStages);
+                }
+                if (ok) commit(smem_u32(&bars->sums_full[use & 1]));
+            }
+        }
+    } else {
+        const int quarter = warp & 3;                         // the lanes of tensor memory that this warp reads
+        T *mine = reinterpret_cast<T *>(store + quarter * 2048);
+        int e = 0, use = 0;
+        bool bad = false;
+        for (int64_t t = pair; t < n_tiles; t += n_pairs, ++use) {
+            const int rt = (int)(t / m_tiles), f0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM + quarter * 32;
+            while (tile_start[e + 1] <= rt) ++e;
+            const int r0 = row_start[e] + (rt - tile_start[e]) * kN, r1 = min(r0 + kN, row_end[e]);
+            const float add = p.bias && f0 + lane < p.features ? p.bias[(int64_t)e * p.features + f0 + lane] : 0.f;
+            if (!warp_wait(smem_u32(&bars->sums_full[use & 1]), (use >> 1) & 1, failed)) break;
+            fence_after();
+            const uint32_t sums = tmem + (use & 1) * kN + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < kN; c += 32) {
+                if (r0 + c >= r1 || f0 >= p.features) break;
+                float v[32];
+                tmem_load32(sums + c, v);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    float z = v[i] + add;
+                    if (!kDx && p.relu) z = z > 0.f || z != z ? z : 0.f;
+                    mine[i * 32 + lane] = from_float<T>(z);
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = i * 32 + lane, r = r0 + c + at / 4, f = f0 + at % 4 * 8;
+                    if (r >= r1 || f >= p.features) continue;
+                    uint4 q = *reinterpret_cast<const uint4 *>(mine + at * 8);
+                    T *z = reinterpret_cast<T *>(&q);
+                    const int n = min(8, p.features - f);
+                    if (kDx && p.mask) {
+                        const int token = p.row_token ? safe_token(p.row_token[r], p.n_tokens, &bad) : r;
+                        const T *x = (const T *)p.mask + token * p.ld_mask + f;
+                        if (n == 8) {
+                            const uint4 xq = *reinterpret_cast<const uint4 *>(x);
+                            const T *xs = reinterpret_cast<const T *>(&xq);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) if (!(to_float(xs[j]) > 0.f)) z[j] = from_float<T>(0.f);
+                        } else {
+                            for (int j = 0; j < n; ++j) if (!(to_float(x[j]) > 0.f)) z[j] = from_float<T>(0.f);
+                        }
+                    }
+                    T *out = (T *)p.out + r * p.ld_out + f;
+                    if (n == 8) *reinterpret_cast<uint4 *>(out) = q;
+                    else for (int j = 0; j < n; ++j) out[j] = z[j];
+                }
+                __syncwarp();
+            }
+            fence_before();
+            if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
+        }
+        if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     }
-    if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+
+    // Both CTAs are done with each other's memory before either leaves; after a failed wait the
+    // copies still under way have to land first.
+    __syncwarp();
+    __syncthreads();
+    if (*failed) {
+        if (threadIdx.x == 0) atomicOr(p.status, (unsigned)GS_DEV_TIMEOUT);
+        const uint64_t start = now_ns();
+        while (now_ns() - start < 1000000ull) { }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp == kWarpMma) tmem_free<S::kTmem>(tmem);
+}
+
+// ---- dW and db --------------------------------------------------------------------------------
+//
+// dW_e: M = out features (dz's columns), N = in features (x's columns), contraction over the
+// expert's rows, 64 at a time.  An expert's rows are cut into equal pieces where it holds more than
+// its share of all rows, so that no pair is left with most of the work; pieces leave their sums in
+// the workspace and a second launch adds them in order.  The tensor cores cut off what does not fit
+// a sum (they do not round), so a long chain of additions drifts towards zero: 2e-6 of the result
+// after 2,048 rows.  A chain therefore ends after kChain steps, and the storing warps add the
+// chains' sums, rounding, in registers (eight warps, half a result row each) while the next chain runs.  Rows past the expert's last one are those
+// of the next expert (or anything at all): warp 6 clears them in shared memory before the matrix
+// instructions may read them.  db is one more product, with a block of ones, for the tiles of the
+// first in features.
+
+constexpr int kMinPiece = 32;                   // steps of 64 rows; an expert is not cut finer
+constexpr int kPiecesPerPair = 2;
+constexpr int kChain = 8;                       // steps
+constexpr int kWeightsStoreWarps = 8, kWarpClear = 2 + kWeightsStoreWarps, kWeightsThreads = 32 * (kWarpClear + 1);
+
+struct WeightsArgs {
+    const int32_t *offsets, *row_token;
+    int n_experts, n_rows, n_tokens, n_out, n_in;
+    float *dw, *db;
+    int64_t ld_dw;
+    float *partial;
+    unsigned *status;
+};
+
+template <int kN> struct WeightsShape {
+    static constexpr uint32_t kBBytes = kN / 2 * 128;
+    static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kN == 256 ? 6 : 8;
+    static constexpr int kStoreBytes = kWeightsStoreWarps * 2048;      // per warp: 32 x 16 floats
+    static constexpr int kOnesBytes = 2048;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + kOnesBytes + sizeof(Barriers) + (5 * GS_MAX_EXPERTS + 8) * sizeof(int);
+    static constexpr int kTmem = 2 * kN;
+    static constexpr int kPartial = kTileM * kN + kTileM;    // floats of one piece: sums, then db
+};
+
+struct Pieces {
+    int *unit_start, *slot_start, *row_start, *row_end, *count;
+};
+
+// Cuts every expert's rows into pieces; units: tiles of pieces, slots: those whose sums are partial.
+__device__ __forceinline__ void scan_pieces(const int32_t *__restrict__ offsets, int n_experts, int n_rows, int tiles, int n_pairs,
+                                            const Pieces &s, int lane) {
+    int64_t steps = 0;
+    int end = 0;
+    for (int base = 0; base < n_experts; base += 32) {
+        const int2 r = ascending_rows(offsets, base + lane, n_experts, n_rows, lane, &end);
+        steps += (r.y - r.x + kDepth - 1) / kDepth;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(kFull, steps, o);
+    const int64_t share = (steps * tiles + n_pairs * kPiecesPerPair - 1) / (n_pairs * kPiecesPerPair);
+    const int most = (int)(share < kMinPiece ? kMinPiece : share);
+    int units = 0, slots = 0;
+    end = 0;
+    for (int base = 0; base < n_experts; base += 32) {
+        const int e = base + lane;
+        const int2 r = ascending_rows(offsets, e, n_experts, n_rows, lane, &end);
+        const int own_steps = (r.y - r.x + kDepth - 1) / kDepth;
+        const int pieces = e < n_experts ? max((own_steps + most - 1) / most, 1) : 0;
+        int u = pieces * tiles, v = pieces > 1 ? pieces * tiles : 0;
+        const int own_u = u, own_v = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up_u = __shfl_up_sync(kFull, u, o), up_v = __shfl_up_sync(kFull, v, o);
+            if (lane >= o) { u += up_u; v += up_v; }
+        }
+        if (e < n_experts) {
+            s.unit_start[e] = units + u - own_u;
+            s.slot_start[e] = slots + v - own_v;
+            s.row_start[e] = r.x;
+            s.row_end[e] = r.y;
+            s.count[e] = pieces;
+        }
+        units += __shfl_sync(kFull, u, 31);
+        slots += __shfl_sync(kFull, v, 31);
+    }
+    if (lane == 0) s.unit_start[n_experts] = units;
+}
+
+// One unit of work: a tile of one piece of an expert's rows.
+struct Unit {
+    int e, piece, m0, n0, first, last, steps, slot;
+};
+__device__ __forceinline__ Unit unit_of(const Pieces &s, int u, int e, int n_tiles_n, int tiles, int kn) {
+    Unit w;
+    const int in_e = u - s.unit_start[e], tile = in_e % tiles;
+    w.e = e;
+    w.piece = in_e / tiles;
+    w.m0 = tile / n_tiles_n * kTileM;
+    w.n0 = tile % n_tiles_n * kn;
+    const int rows = s.row_end[e] - s.row_start[e], steps = (rows + kDepth - 1) / kDepth, pieces = s.count[e];
+    const int per = (steps + pieces - 1) / pieces, s0 = min(w.piece * per, steps), s1 = min(s0 + per, steps);
+    w.steps = s1 - s0;
+    w.first = s.row_start[e] + s0 * kDepth;
+    w.last = min(s.row_start[e] + s1 * kDepth, s.row_end[e]);
+    w.slot = pieces > 1 ? s.slot_start[e] + in_e : -1;
+    return w;
+}
+
+template <typename T, int kN, bool kGather>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWeightsThreads, 1)
+weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant__ CUtensorMap map_x, const WeightsArgs p)
+{
+    using S = WeightsShape<kN>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    unsigned char *ones = smem + S::kStages * S::kStageBytes, *store = ones + S::kOnesBytes;
+    Barriers *bars = reinterpret_cast<Barriers *>(store + S::kStoreBytes);
+    Pieces s;
+    s.unit_start = reinterpret_cast<int *>(bars + 1);
+    s.slot_start = s.unit_start + GS_MAX_EXPERTS + 1;
+    s.row_start = s.slot_start + GS_MAX_EXPERTS;
+    s.row_end = s.row_start + GS_MAX_EXPERTS;
+    s.count = s.row_end + GS_MAX_EXPERTS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    volatile int *failed = &bars->failed;
+    const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+    const int tiles_n = (p.n_in + kN - 1) / kN, tiles = tiles_n * ((p.n_out + kTileM - 1) / kTileM);
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    setup_pair(bars, S::kStages, kWeightsStoreWarps, warp, lane);
+    if (warp == kWarpMma) tmem_alloc<S::kTmem>(smem_u32(&bars->tmem));
+    if (p.db) {
+        for (int i = threadIdx.x; i < S::kOnesBytes / 2; i += blockDim.x) reinterpret_cast<T *>(ones)[i] = from_float<T>(1.f);
+        fence_async_smem();
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0) scan_pieces(p.offsets, p.n_experts, p.n_rows, tiles, n_pairs, s, lane);
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+
+    const uint32_t tmem = bars->tmem;
+    const int n_units = s.unit_start[p.n_experts];
+
+    if (warp == kWarpProducer) {
+        if (lane == 0) { prefetch_map(&map_dz); prefetch_map(&map_x); }
+        Ring ring;
+        int e = 0;
+        bool bad = false, ok = true;
+        for (int u = pair; u < n_units && ok; u += n_pairs) {
+            while (s.unit_start[e + 1] <= u) ++e;
+            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+            const int a0 = w.m0 + (int)rank * kHalfM, b0 = w.n0 + (int)rank * (kN / 2);
+            int token[4];
+            if (kGather && w.steps > 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(w.first + lane % 16 * 4 + i, w.last - 1)];
+            }
+            for (int k = 0; k < w.steps; ++k) {
+                const int r = w.first + k * kDepth;
+                const bool tail = r + kDepth > w.last;       // the clearing warp passes this step on
+                if (!warp_wait(smem_u32(&bars->empty[ring.stage]), ring.round ^ 1, failed)) { ok = false; break; }
+                const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes), b = a + kABytes;
+                // (a step that has to be cleared lands on this CTA's own barrier; an address of the CTA itself is one of the cluster too)
+                const uint32_t full = tail ? smem_u32(&bars->landed[ring.stage]) : in_leader(smem_u32(&bars->full[ring.stage]));
+                if (lane == 0) {
+                    bar_expect(full, S::kStageBytes);
+                    copy_2d(&map_dz, a, full, a0, r);
+                    copy_2d(&map_dz, a + kABytes / 2, full, a0 + 64, r);
+                    if (!kGather)
+#pragma unroll
+                        for (int i = 0; i < kN / 128; ++i) copy_2d(&map_x, b + i * 8192, full, b0 + i * 64, r);
+                }
+                if (kGather) {
+                    int t[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[i] = safe_token(token[i], p.n_tokens, &bad);
+                    if (k + 1 < w.steps) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(r + kDepth + lane % 16 * 4 + i, w.last - 1)];
+                    }
+                    __syncwarp();
+                    // sixteen groups of four rows, kN / 128 columns of boxes, dealt out to the lanes
+                    for (int i = lane / 16; i < kN / 128; i += 2)
+                        copy_rows4(&map_x, b + i * 8192 + lane % 16 * 512, full, b0 + i * 64, t[0], t[1], t[2], t[3]);
+                }
+                ring.next(S::kStages);
+            }
+        }
+        if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
+    } else if (warp == kWarpMma) {
+        if (rank == 0 && lane == 0) {
+            constexpr uint32_t kInstr = instruction(kBf16<T>, true, true, kTileM, kN);
+            constexpr uint32_t kInstrOnes = instruction(kBf16<T>, true, true, kTileM, 32);
+            const uint64_t d_ones = operand(smem_u32(ones), 16);
+            Ring ring;
+            int use = 0, e = 0;
+            bool ok = true;
+            for (int u = pair; u < n_units && ok; u += n_pairs) {
+                while (s.unit_start[e + 1] <= u) ++e;
+                const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+                if (w.steps == 0) continue;
+                const bool with_db = p.db && w.n0 == 0;
+                for (int k0 = 0; k0 < w.steps && ok; k0 += kChain) {
+                    const uint32_t sums = tmem + (use & 1) * kN, other = tmem + (~use & 1) * kN;
+                    if (!bar_wait(smem_u32(&bars->sums_empty[use & 1]), ((use >> 1) & 1) ^ 1, failed) ||
+                        (with_db && !bar_wait(smem_u32(&bars->sums_empty[~use & 1]), (((use + 1) >> 1) & 1) ^ 1, failed))) {
+                        ok = false;
+                        break;
+                    }
+                    fence_after();
+                    const int k1 = min(k0 + kChain, w.steps);
+                    for (int k = k0; k < k1; ++k) {
+                        if (!bar_wait(smem_u32(&bars->full[ring.stage]), ring.round, failed)) { ok = false; break; }
+                        fence_after();
+                        const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes);
+                        const uint64_t da = operand(a, kABytes / 2), db = operand(a + kABytes, 8192);
+#pragma unroll
+                        for (int i = 0; i < kDepth / 16; ++i) {
+                            mma(sums, da + i * 2048 / 16, db + i * 2048 / 16, kInstr, k > k0 || i > 0);
+                            if (with_db) mma(other, da + i * 2048 / 16, d_ones, kInstrOnes, k > k0 || i > 0);
+                        }
+                        commit(smem_u32(&bars->empty[ring.stage]));
+                        ring.next(S::kStages);
+                    }
+                    if (!ok) break;
+                    commit(smem_u32(&bars->sums_full[use & 1]));
+                    ++use;
+                    if (with_db) { commit(smem_u32(&bars->sums_full[use & 1])); ++use; }
+                }
+            }
+        }
+    } else if (warp == kWarpClear) {
+        Ring ring;
+        int e = 0;
+        unsigned rounds = 0;                                 // bit s: parity of stage s's next landing
+        bool ok = true;
+        for (int u = pair; u < n_units && ok; u += n_pairs) {
+            while (s.unit_start[e + 1] <= u) ++e;
+            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+            for (int k = 0; k < w.steps; ++k) {
+                const int left = w.last - (w.first + k * kDepth);
+                if (left < kDepth) {
+                    if (!warp_wait(smem_u32(&bars->landed[ring.stage]), (rounds >> ring.stage) & 1, failed)) { ok = false; break; }
+                    rounds ^= 1u << ring.stage;
+                    unsigned char *box = smem + ring.stage * S::kStageBytes;
+                    const int bytes = (kDepth - left) * 128;
+                    for (int i = 0; i < (int)(S::kStageBytes / 8192); ++i)
+                        for (int at = lane * 16; at < bytes; at += 512)
+                            *reinterpret_cast<uint4 *>(box + i * 8192 + left * 128 + at) = make_uint4(0, 0, 0, 0);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->full[ring.stage])));
+                }
+                ring.next(S::kStages);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;       // lanes of tensor memory, columns of the tile
+        constexpr int kCols = kN / 2;
+        float *mine = reinterpret_cast<float *>(store + (warp - 2) * 2048);
+        const uint32_t sums = tmem + ((uint32_t)(quarter * 32) << 16);
+        int use = 0, e = 0;
+        bool ok = true;
+        for (int u = pair; u < n_units && ok; u += n_pairs) {
+            while (s.unit_start[e + 1] <= u) ++e;
+            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+            const int row = (int)rank * kHalfM + quarter * 32, o0 = w.m0 + row;      // this warp's rows in the tile and in dW
+            const bool with_db = p.db && w.n0 == 0;
+            float v[kCols], bias = 0.f;
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) v[i] = 0.f;
+            for (int k = 0; k < w.steps; k += kChain) {
+                if (!warp_wait(smem_u32(&bars->sums_full[use & 1]), (use >> 1) & 1, failed)) { ok = false; break; }
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < kCols; c += 16) {
+                    float q[16];
+                    tmem_load16(sums + (use & 1) * kN + half * kCols + c, q);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[c + i] += q[i];
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
+                ++use;
+                if (!with_db) continue;
+                if (!warp_wait(smem_u32(&bars->sums_full[use & 1]), (use >> 1) & 1, failed)) { ok = false; break; }
+                fence_after();
+                bias += tmem_load1(sums + (use & 1) * kN);
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
+                ++use;
+            }
+            if (!ok) break;
+            if (w.slot >= 0) {                                // four columns of every row, then the next four
+                float *part = p.partial + (int64_t)w.slot * S::kPartial;
+#pragma unroll
+                for (int i = 0; i < kCols / 4; ++i)
+                    *reinterpret_cast<float4 *>(part + ((int64_t)(half * (kCols / 4) + i) * kTileM + row + lane) * 4) =
+                        make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                if (with_db && half == 0) part[kTileM * kN + row + lane] = bias;
+                continue;
+            }
+            if (with_db && half == 0 && o0 + lane < p.n_out) p.db[(int64_t)w.e * p.n_out + o0 + lane] = bias;
+            // through shared memory, so that a warp writes 64-byte stretches of rows
+#pragma unroll
+            for (int c = 0; c < kCols; c += 16) {
+                const int col0 = w.n0 + half * kCols + c;
+                if (o0 >= p.n_out || col0 >= p.n_in) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4 *>(mine + lane * 16 + ((i ^ (lane >> 1)) & 3) * 4) =
+                        make_float4(v[c + 4 * i], v[c + 4 * i + 1], v[c + 4 * i + 2], v[c + 4 * i + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = i * 8 + lane / 4, col = col0 + lane % 4 * 4;
+                    const float4 q = *reinterpret_cast<const float4 *>(mine + at * 16 + ((lane ^ (at >> 1)) & 3) * 4);
+                    if (o0 + at < p.n_out && col < p.n_in) {
+                        float *out = p.dw + ((int64_t)w.e * p.n_out + o0 + at) * p.ld_dw + col;
+                        if (col + 4 <= p.n_in) *reinterpret_cast<float4 *>(out) = q;
+                        else {
+                            out[0] = q.x;
+                            if (col + 1 < p.n_in) out[1] = q.y;
+                            if (col + 2 < p.n_in) out[2] = q.z;
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+
+    __syncwarp();
+    __syncthreads();
+    if (*failed) {
+        if (threadIdx.x == 0) atomicOr(p.status, (unsigned)GS_DEV_TIMEOUT);
+        const uint64_t start = now_ns();
+        while (now_ns() - start < 1000000ull) { }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp == kWarpMma) tmem_free<S::kTmem>(tmem);
+}
+
+// Adds up the pieces of the experts that were cut, in order.  A CTA takes 32 rows of a tile.
+template <int kN>
+__global__ void __launch_bounds__(256)
+weights_sum_kernel(const WeightsArgs p, int n_pairs)
+{
+    using S = WeightsShape<kN>;
+    __shared__ int tables[5 * GS_MAX_EXPERTS + 1];
+    dependent_begin();
+    Pieces s = {tables, tables + GS_MAX_EXPERTS + 1, tables + 2 * GS_MAX_EXPERTS + 1, tables + 3 * GS_MAX_EXPERTS + 1, tables + 4 * GS_MAX_EXPERTS + 1};
+    const int tiles_n = (p.n_in + kN - 1) / kN, tiles = tiles_n * ((p.n_out + kTileM - 1) / kTileM);
+    if (threadIdx.x < 32) scan_pieces(p.offsets, p.n_experts, p.n_rows, tiles, n_pairs, s, threadIdx.x);
+    __syncthreads();
+    constexpr int kParts = kTileM / 32;
+    int before = 0;                                          // cut tiles of the experts before e
+    int64_t job = blockIdx.x;
+    for (int e = 0; e < p.n_experts; ++e) {
+        if (s.count[e] < 2) continue;
+        for (; job < (int64_t)(before + tiles) * kParts; job += gridDim.x) {
+            const int tile = (int)(job / kParts) - before, part = (int)(job % kParts);
+            const int m0 = tile / tiles_n * kTileM, n0 = tile % tiles_n * kN;
+            const float *base = p.partial + ((int64_t)s.slot_start[e] + tile) * S::kPartial;
+            for (int i = threadIdx.x; i < 32 * (kN / 4); i += 256) {
+                const int row = part * 32 + i / (kN / 4), col4 = i % (kN / 4), o = m0 + row, col = n0 + col4 * 4;
+                if (o >= p.n_out || col >= p.n_in) continue;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int piece = 0; piece < s.count[e]; ++piece) {
+                    const float4 q = *reinterpret_cast<const float4 *>(base + (int64_t)piece * tiles * S::kPartial + ((int64_t)col4 * kTileM + row) * 4);
+                    sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
+                }
+                float *out = p.dw + ((int64_t)e * p.n_out + o) * p.ld_dw + col;
+                if (col + 4 <= p.n_in) *reinterpret_cast<float4 *>(out) = sum;
+                else {
+                    out[0] = sum.x;
+                    if (col + 1 < p.n_in) out[1] = sum.y;
+                    if (col + 2 < p.n_in) out[2] = sum.z;
+                }
+            }
+            if (p.db && n0 == 0 && threadIdx.x < 32 && m0 + part * 32 + (int)threadIdx.x < p.n_out) {
+                const int row = part * 32 + threadIdx.x;
+                float sum = 0.f;
+                for (int piece = 0; piece < s.count[e]; ++piece) sum += base[(int64_t)piece * tiles * S::kPartial + kTileM * kN + row];
+                p.db[(int64_t)e * p.n_out + m0 + row] = sum;
+            }
+        }
+        before += tiles;
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled g_encode = nullptr;
+
+// Tensor map of 16-bit values whose boxes are 64 wide (128 bytes, swizzled) and `box_rows` high.
+bool encode(CUtensorMap *map, int dtype, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, int box_rows) {
+    const cuuint32_t box[3] = {(cuuint32_t)kDepth, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    return g_encode(map, dtype == GS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+                    const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_matrix(CUtensorMap *map, int dtype, const void *base, int64_t rows, int64_t ld, int cols, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    return encode(map, dtype, base, 2, dims, strides, box_rows);
+}
+
+bool encode_weights(CUtensorMap *map, const ExpertLinearArgs &a, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)a.in, (cuuint64_t)a.out, (cuuint64_t)a.n_experts};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.ld_w * 2, (cuuint64_t)a.ld_w * 2 * a.out};
+    return encode(map, a.dtype, a.w, 3, dims, strides, box_rows);
+}
+
+int pairs_of(const gs_ctx *ctx) { return ctx->n_sm / 2; }
+
+// Calls f with the width of the N tile: the widest that the average expert fills well.
+template <typename F> cudaError_t by_rows(const ExpertLinearArgs &a, F &&f) {
+    const int64_t each = a.n_rows / a.n_experts;
+    if (each >= 160) return f(std::integral_constant<int, 256>());
+    if (each >= 80) return f(std::integral_constant<int, 128>());
+    if (each >= 40) return f(std::integral_constant<int, 64>());
+    return f(std::integral_constant<int, 32>());
+}
+
+template <typename T, bool kDx, int kN, bool kGather>
+cudaError_t launch_rows(gs_ctx *ctx, const CUtensorMap &map_w, const CUtensorMap &map_x, const RowsArgs &p, cudaStream_t st) {
+    const int64_t tiles = (p.n_rows / kN + p.n_experts) * (int64_t)((p.features + kTileM - 1) / kTileM);
+    const int pairs = (int)(tiles < pairs_of(ctx) ? tiles : pairs_of(ctx));
+    LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
+    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
 }
 
 template <typename T> cudaError_t forward_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
-    const dim3 grid((unsigned)((a.n_rows + kTile - 1) / kTile + a.n_experts), (a.out + kTile - 1) / kTile);
-    LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(rows_kernel<T, false>, grid, dim3(kThreads), 0, st, (const T *)a.x, a.ld_x, a.row_token,
-                            (int)a.n_x_rows, a.offsets, a.n_experts, (int)a.n_rows, (const T *)a.w, a.ld_w, a.out, a.in,
-                            a.out, a.bias, (a.flags & GS_EXPERT_RELU) != 0, (const T *)nullptr, (int64_t)0, (const int32_t *)nullptr, 0,
-                            (T *)a.y, a.ld_y, ctx->s.status);
+    RowsArgs p = {a.offsets, a.row_token, a.n_experts, (int)a.n_rows, (int)a.n_x_rows, a.out, a.in, a.bias,
+                  (a.flags & GS_EXPERT_RELU) != 0, nullptr, 0, a.y, a.ld_y, ctx->s.status};
+    return by_rows(a, [&](auto width) {
+        constexpr int N = decltype(width)::value;
+        CUtensorMap map_w, map_x;
+        if (!encode_weights(&map_w, a, kHalfM) ||
+            !encode_matrix(&map_x, a.dtype, a.x, a.n_x_rows, a.ld_x, a.in, a.row_token ? 1 : N / 2)) return cudaErrorInvalidValue;
+        return a.row_token ? launch_rows<T, false, N, true>(ctx, map_w, map_x, p, st) : launch_rows<T, false, N, false>(ctx, map_w, map_x, p, st);
+    });
 }
 
 template <typename T> cudaError_t dx_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
-    const dim3 grid((unsigned)((a.n_rows + kTile - 1) / kTile + a.n_experts), (a.in + kTile - 1) / kTile);
-    const bool masked = a.flags & GS_EXPERT_RELU_INPUT;
-    LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(rows_kernel<T, true>, grid, dim3(kThreads), 0, st, (const T *)a.dz, a.ld_dz, (const int32_t *)nullptr,
-                            0, a.offsets, a.n_experts, (int)a.n_rows, (const T *)a.w, a.ld_w, a.out, a.out,
-                            a.in, (const float *)nullptr, false, masked ? (const T *)a.x : (const T *)nullptr, a.ld_x, a.row_token, (int)a.n_x_rows,
-                            (T *)a.dx, a.ld_dx, ctx->s.status);
+    const bool masked = (a.flags & GS_EXPERT_RELU_INPUT) != 0;
+    RowsArgs p = {a.offsets, a.row_token, a.n_experts, (int)a.n_rows, (int)a.n_x_rows, a.in, a.out, nullptr, false,
+                  masked ? a.x : nullptr, a.ld_x, a.dx, a.ld_dx, ctx->s.status};
+    return by_rows(a, [&](auto width) {
+        constexpr int N = decltype(width)::value;
+        CUtensorMap map_w, map_dz;
+        if (!encode_weights(&map_w, a, kDepth) || !encode_matrix(&map_dz, a.dtype, a.dz, a.n_rows, a.ld_dz, a.out, N / 2)) return cudaErrorInvalidValue;
+        return launch_rows<T, true, N, false>(ctx, map_w, map_dz, p, st);
+    });
 }
 
-template <typename T> cudaError_t dw_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
-    const dim3 grid((a.in + kTile - 1) / kTile, (a.out + kTile - 1) / kTile, a.n_experts);
+int weights_tile(int in) { return in > 128 ? 256 : 128; }
+
+template <typename T, int kN> cudaError_t dw_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
+    if (a.n_rows == 0) {
+        cudaError_t e = cudaMemset2DAsync(a.dw, (size_t)a.ld_dw * 4, 0, (size_t)a.in * 4, (size_t)a.n_experts * a.out, st);
+        if (e == cudaSuccess && a.db) e = cudaMemsetAsync(a.db, 0, (size_t)a.n_experts * a.out * 4, st);
+        return e;
+    }
+    const WeightsArgs p = {a.offsets, a.row_token, a.n_experts, (int)a.n_rows, (int)a.n_x_rows, a.out, a.in, a.dw, a.db, a.ld_dw,
+                           (float *)a.workspace, ctx->s.status};
+    CUtensorMap map_dz, map_x;
+    if (!encode_matrix(&map_dz, a.dtype, a.dz, a.n_rows, a.ld_dz, a.out, kDepth) ||
+        !encode_matrix(&map_x, a.dtype, a.x, a.n_x_rows, a.ld_x, a.in, a.row_token ? 1 : kDepth)) return cudaErrorInvalidValue;
+    const int pairs = pairs_of(ctx);
+    cudaError_t e;
+    {
+        LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
+        e = a.row_token ? launch_dependent(weights_kernel<T, kN, true>, dim3(2 * pairs), dim3(kWeightsThreads), WeightsShape<kN>::kSmem, st, map_dz, map_x, p)
+                        : launch_dependent(weights_kernel<T, kN, false>, dim3(2 * pairs), dim3(kWeightsThreads), WeightsShape<kN>::kSmem, st, map_dz, map_x, p);
+    }
+    if (e != cudaSuccess || expert_linear_workspace(ctx, a.n_experts, a.n_rows, a.in, a.out) == 0) return e;
     LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(weights_kernel<T>, grid, dim3(kThreads), 0, st, (const T *)a.dz, a.ld_dz, (const T *)a.x, a.ld_x,
-                            a.row_token, (int)a.n_x_rows, a.offsets, (int)a.n_rows, a.out, a.in, a.dw, a.ld_dw, a.db, ctx->s.status);
+    return launch_dependent(weights_sum_kernel<kN>, dim3(4 * ctx->n_sm), dim3(256), 0, st, p, pairs);
+}
+
+template <typename T> cudaError_t dw_by_tile(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
+    return weights_tile(a.in) == 256 ? dw_as<T, 256>(ctx, a, st) : dw_as<T, 128>(ctx, a, st);
+}
+
+template <typename T, int kN> cudaError_t configure_rows() {
+    cudaError_t e = cudaFuncSetAttribute(rows_kernel<T, false, kN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<kN>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rows_kernel<T, false, kN, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<kN>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rows_kernel<T, true, kN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RowsShape<kN>::kSmem);
+    return e;
+}
+
+template <typename T, int kN> cudaError_t configure_weights() {
+    cudaError_t e = cudaFuncSetAttribute(weights_kernel<T, kN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WeightsShape<kN>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_kernel<T, kN, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WeightsShape<kN>::kSmem);
+    return e;
+}
+
+template <typename T> cudaError_t configure_as() {
+    for (auto f : {configure_rows<T, 32>, configure_rows<T, 64>, configure_rows<T, 128>, configure_rows<T, 256>, configure_weights<T, 128>, configure_weights<T, 256>}) {
+        const cudaError_t e = f();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
 
-cudaError_t configure_expert_linear() { return cudaSuccess; }
-int64_t expert_linear_workspace(const gs_ctx *, int, int64_t, int, int) { return 0; }
+cudaError_t configure_expert_linear() {
+    void *f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return e;
+    if (found != cudaDriverEntryPointSuccess || !f) return cudaErrorNotSupported;
+    g_encode = reinterpret_cast<EncodeTiled>(f);
+    e = configure_as<__nv_bfloat16>();
+    return e == cudaSuccess ? configure_as<__half>() : e;
+}
+
+// An expert is cut only if it has more steps than kMinPiece and than a share (the whole work over
+// kPiecesPerPair pieces per pair); it then has at most 2 * steps / share pieces, and all cut
+// experts together at most twice the number of shares.
+int64_t expert_linear_workspace(const gs_ctx *ctx, int, int64_t n_rows, int in, int) {
+    if (n_rows <= kMinPiece * kDepth) return 0;
+    return 2 * (int64_t)pairs_of(ctx) * kPiecesPerPair * (kTileM * weights_tile(in) + kTileM) * 4;
+}
 
 cudaError_t launch_expert_linear(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
     return a.dtype == GS_BF16 ? forward_as<__nv_bfloat16>(ctx, a, st) : forward_as<__half>(ctx, a, st);
@@ -178,7 +835,7 @@ cudaError_t launch_expert_linear_dx(gs_ctx *ctx, const ExpertLinearArgs &a, cuda
     return a.dtype == GS_BF16 ? dx_as<__nv_bfloat16>(ctx, a, st) : dx_as<__half>(ctx, a, st);
 }
 cudaError_t launch_expert_linear_dw(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
-    return a.dtype == GS_BF16 ? dw_as<__nv_bfloat16>(ctx, a, st) : dw_as<__half>(ctx, a, st);
+    return a.dtype == GS_BF16 ? dw_by_tile<__nv_bfloat16>(ctx, a, st) : dw_by_tile<__half>(ctx, a, st);
 }
 
 }  // namespace gs

@@ -39,11 +39,6 @@ __device__ __forceinline__ void dependent_begin() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Rows of expert e, from offsets that may be anything (they are clamped into [0, n_rows]).
-__device__ __forceinline__ int2 expert_rows(const int32_t *__restrict__ offsets, int e, int n_rows) {
-    const int a = min(max(offsets[e], 0), n_rows), b = min(max(offsets[e + 1], a), n_rows);
-    return make_int2(a, b);
-}
 
 struct ExpertRouteArgs {
     const void *logits;
