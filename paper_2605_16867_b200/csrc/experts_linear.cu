@@ -545,7 +545,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
                             *reinterpret_cast<uint4 *>(box + i * 8192 + left * 128 + at) = make_uint4(0, 0, 0, 0);
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->full[ring.stage])));
+                    if (lane == 0) bar_arrive_release(in_leader(smem_u32(&bars->full[ring.stage])));
                 }
                 ring.next(S::kStages);
             }
