@@ -128,7 +128,7 @@ template <int kN> struct RowsShape {
 
 // kDx: the weights' tile has its features contiguous (the contraction runs over their rows).
 template <typename T, bool kDx, int kN, bool kGather>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(192, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 288 : 192, 1)
 rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const RowsArgs p)
 {
     using S = RowsShape<kN>;
@@ -156,8 +156,9 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     const int64_t n_tiles = (int64_t)tile_start[p.n_experts] * m_tiles;
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
-    if (warp == kWarpProducer) {
-        if (lane == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
+    if (warp == kWarpProducer || warp >= 6) {
+        const int helper = warp == kWarpProducer ? 0 : warp - 5;     // four warps share out the gathered rows
+        if (threadIdx.x == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
         Ring ring;
         int e = 0;
         bool bad = false, ok = true;
@@ -165,22 +166,19 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             const int rt = (int)(t / m_tiles), m0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM;
             while (tile_start[e + 1] <= rt) ++e;
             const int r0 = row_start[e] + (rt - tile_start[e]) * kN + (int)rank * (kN / 2);
-            constexpr int kGroups = (kN / 2 + 127) / 128;      // of four rows per lane
-            int token[kGroups][4];
-            if (kGather) {
+            constexpr int kLanes = kN / 32;                    // of each warp: four rows per lane
+            const int row = (helper * kLanes + lane) * 4;
+            int token[4];
+            if (kGather && lane < kLanes) {
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = min(r0 + (g * 32 + lane) * 4 + i, row_end[e] - 1);
-                        token[g][i] = safe_token(p.row_token[r], p.n_tokens, &bad);
-                    }
+                for (int i = 0; i < 4; ++i)
+                    token[i] = safe_token(p.row_token[min(r0 + row + i, row_end[e] - 1)], p.n_tokens, &bad);
             }
             for (int k = 0; k < k_steps; ++k) {
                 if (!warp_wait(smem_u32(&bars->empty[ring.stage]), ring.round ^ 1, failed)) { ok = false; break; }
                 const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes), b = a + kABytes;
                 const uint32_t full = in_leader(smem_u32(&bars->full[ring.stage]));
-                if (lane == 0) {
+                if (lane == 0 && helper == 0) {
                     bar_expect(full, S::kStageBytes);
                     if (kDx) {
                         copy_3d(&map_w, a, full, m0, k * kDepth, e);
@@ -190,15 +188,8 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                     }
                     if (!kGather) copy_2d(&map_x, b, full, k * kDepth, r0);
                 }
-                if (kGather) {
-                    __syncwarp();
-#pragma unroll
-                    for (int g = 0; g < kGroups; ++g) {
-                        const int row = (g * 32 + lane) * 4;
-                        if (row < kN / 2)
-                            copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[g][0], token[g][1], token[g][2], token[g][3]);
-                    }
-                }
+                if (kGather && lane < kLanes) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
+                __syncwarp();
                 ring.next(S::kStages);
             }
         }
@@ -730,7 +721,7 @@ cudaError_t launch_rows(gs_ctx *ctx, const CUtensorMap &map_w, const CUtensorMap
     const int64_t tiles = (p.n_rows / kN + p.n_experts) * (int64_t)((p.features + kTileM - 1) / kTileM);
     const int pairs = (int)(tiles < pairs_of(ctx) ? tiles : pairs_of(ctx));
     LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
+    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(kGather ? 288 : 192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
 }
 
 template <typename T> cudaError_t forward_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
