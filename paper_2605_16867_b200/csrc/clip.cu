@@ -31,16 +31,77 @@ __device__ __forceinline__ int tensor_of(const ClipTable &t, int chunk) {
     return lo;
 }
 
+// Sixteen bytes of T.
+template <typename T> struct Pack {
+    static constexpr int kN = 16 / (int)sizeof(T);
+    uint4 q;
+    __device__ __forceinline__ float at(int i) const { return to_float(reinterpret_cast<const T *>(&q)[i]); }
+    __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T *>(&q)[i] = from_float<T>(v); }
+};
+
+// Squares of 16 bytes of gradients.  A float holds their sum unless it is very large, very small or
+// not a number; then the squares are taken in double (a conversion per value is what would bound
+// the kernel otherwise).
+template <typename T>
+__device__ __forceinline__ double pack_square(const Pack<T> &g) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < Pack<T>::kN; ++i) sum = fmaf(g.at(i), g.at(i), sum);
+    if ((sum >= 1e-24f && sum <= 1e38f) || (g.q.x | g.q.y | g.q.z | g.q.w) == 0u) return (double)sum;
+    double wide = 0.0;
+#pragma unroll
+    for (int i = 0; i < Pack<T>::kN; ++i) wide = fma((double)g.at(i), (double)g.at(i), wide);
+    return wide;
+}
+
+// Elements before the first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ int to_boundary(const T *p, int n) {
+    return min((int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(T)), n);
+}
+
 template <typename T>
 __device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
+    constexpr int kN = Pack<T>::kN, kAhead = 4;
+    const int head = to_boundary(g, n), packs = (n - head) / kN, tail = head + packs * kN;
+    const uint4 *q = reinterpret_cast<const uint4 *>(g + head);
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += kClipThreads) { const double v = (double)to_float(g[i]); sum = fma(v, v, sum); }
+    for (int i = threadIdx.x; i < packs; i += kAhead * kClipThreads) {
+        Pack<T> v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            v[k].q = i + k * kClipThreads < packs ? __ldg(q + i + k * kClipThreads) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) sum += pack_square(v[k]);
+    }
+    const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
+    if (edge < n) { const double v = (double)to_float(g[edge]); sum = fma(v, v, sum); }
     return sum;
 }
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T *g, T *out, int n, float f) {
-    for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(to_float(g[i]) * f);
+    constexpr int kN = Pack<T>::kN, kAhead = 4;
+    if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
+        for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(to_float(g[i]) * f);
+        return;
+    }
+    const int head = to_boundary(g, n), packs = (n - head) / kN, tail = head + packs * kN;
+    const uint4 *q = reinterpret_cast<const uint4 *>(g + head);
+    uint4 *o = reinterpret_cast<uint4 *>(out + head);
+    for (int i = threadIdx.x; i < packs; i += kAhead * kClipThreads) {
+        Pack<T> v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) if (i + k * kClipThreads < packs) v[k].q = q[i + k * kClipThreads];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+#pragma unroll
+            for (int j = 0; j < kN; ++j) v[k].set(j, v[k].at(j) * f);
+            if (i + k * kClipThreads < packs) o[i + k * kClipThreads] = v[k].q;
+        }
+    }
+    const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
+    if (edge < n) out[edge] = from_float<T>(to_float(g[edge]) * f);
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -92,8 +153,10 @@ clip_kernel(const __grid_constant__ ClipTable t, const double *__restrict__ part
 {
     dependent_begin();
     const float f = clip_factor(partials, n_partials, max_norm, out_norm, status);
-    for (int c = blockIdx.x; c < t.chunk_start[t.n]; c += gridDim.x) {
+    // the other way round: what the norm read last is still in L2
+    for (int c = t.chunk_start[t.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const int k = tensor_of(t, c);
+        if (f == 1.f && t.grad[k] == t.out[k]) continue;
         const int64_t first = (int64_t)(c - t.chunk_start[k]) * kClipChunk;
         const int n = (int)min((int64_t)kClipChunk, t.n_elements[k] - first);
         if (t.dtype[k] == GS_F32) chunk_scale((const float *)t.grad[k] + first, (float *)t.out[k] + first, n, f);

@@ -28,6 +28,10 @@ constexpr int kTileM = 2 * kHalfM;
 constexpr uint32_t kABytes = kHalfM * 128;
 constexpr int kWarpProducer = 0, kWarpMma = 1;      // the next four (eight in dW) store, dW's last one clears
 constexpr int kMaxStages = 10;
+// A gather instruction fetches four rows, one lane at a time; one warp issues them in some 75 cycles
+// each, far below what the copies could carry.  131,072 requests of the first layer with 1 / 4 / 8 /
+// 16 warps: 2,160 / 970 / 889 / 877 us.
+constexpr int kGatherWarps = 8;
 
 struct Barriers {
     uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], sums_full[2], sums_empty[2];
@@ -128,7 +132,7 @@ template <int kN> struct RowsShape {
 
 // kDx: the weights' tile has its features contiguous (the contraction runs over their rows).
 template <typename T, bool kDx, int kN, bool kGather>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 288 : 192, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 160 + 32 * kGatherWarps : 192, 1)
 rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const RowsArgs p)
 {
     using S = RowsShape<kN>;
@@ -157,7 +161,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
     if (warp == kWarpProducer || warp >= 6) {
-        const int helper = warp == kWarpProducer ? 0 : warp - 5;     // four warps share out the gathered rows
+        const int helper = warp == kWarpProducer ? 0 : warp - 5;     // kGatherWarps warps share out the gathered rows
         if (threadIdx.x == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
         Ring ring;
         int e = 0;
@@ -166,10 +170,10 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             const int rt = (int)(t / m_tiles), m0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM;
             while (tile_start[e + 1] <= rt) ++e;
             const int r0 = row_start[e] + (rt - tile_start[e]) * kN + (int)rank * (kN / 2);
-            constexpr int kLanes = kN / 32;                    // of each warp: four rows per lane
+            constexpr int kLanes = kN >= 8 * kGatherWarps ? kN / (8 * kGatherWarps) : 1;     // of each warp: four rows per lane
             const int row = (helper * kLanes + lane) * 4;
             int token[4];
-            if (kGather && lane < kLanes) {
+            if (kGather && lane < kLanes && row < kN / 2) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     token[i] = safe_token(p.row_token[min(r0 + row + i, row_end[e] - 1)], p.n_tokens, &bad);
@@ -188,7 +192,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                     }
                     if (!kGather) copy_2d(&map_x, b, full, k * kDepth, r0);
                 }
-                if (kGather && lane < kLanes) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
+                if (kGather && lane < kLanes && row < kN / 2) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
                 __syncwarp();
                 ring.next(S::kStages);
             }
@@ -721,7 +725,7 @@ cudaError_t launch_rows(gs_ctx *ctx, const CUtensorMap &map_w, const CUtensorMap
     const int64_t tiles = (p.n_rows / kN + p.n_experts) * (int64_t)((p.features + kTileM - 1) / kTileM);
     const int pairs = (int)(tiles < pairs_of(ctx) ? tiles : pairs_of(ctx));
     LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(kGather ? 288 : 192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
+    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(kGather ? 160 + 32 * kGatherWarps : 192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
 }
 
 template <typename T> cudaError_t forward_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {

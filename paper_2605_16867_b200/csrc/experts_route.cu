@@ -50,26 +50,52 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// A row's logits, expert i * 32 + lane in element i; -infinity where there is none to choose.
+// Logits as the definition reads them: NaN takes the expert out, +infinity is the largest finite number.
+__device__ __forceinline__ float clean_logit(float v, bool *nan) {
+    if (v != v) { *nan = true; return -INFINITY; }
+    return fminf(v, kLargest);
+}
+
+// 1 / (1 + exp(-x)); the reciprocal is the approximate one (1 ulp).  0 at -infinity.
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+
+// A row's logits, experts lane * V .. lane * V + V - 1; -infinity where there is none to choose.
+// `whole`: rows start so aligned, and experts divide so evenly, that a lane's can be read at once.
 template <typename T, int V>
-__device__ __forceinline__ bool load_row(const T *__restrict__ row, int n_experts, int lane, float (&x)[V]) {
-    bool nan = false;
+__device__ __forceinline__ void load_row(const T *__restrict__ row, int n_experts, int lane, bool whole, float (&x)[V], bool *nan) {
+    const int first = lane * V;
+    if (whole) {
+        constexpr int kBytes = V * sizeof(T) < 16 ? V * sizeof(T) : 16, kEach = kBytes / sizeof(T);
+        using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, unsigned, unsigned short>>>;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = i * 32 + lane;
-        float v = e < n_experts ? to_float(row[e]) : -INFINITY;
-        if (v != v) { nan = true; v = -INFINITY; }
-        x[i] = fminf(v, kLargest);
+        for (int w = 0; w < V / kEach; ++w) {
+            if (first < n_experts) {
+                const Word q = reinterpret_cast<const Word *>(row + first)[w];
+                const T *t = reinterpret_cast<const T *>(&q);
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = clean_logit(to_float(t[i]), nan);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = -INFINITY;
+            }
+        }
+        return;
     }
-    return nan;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = first + i < n_experts ? clean_logit(to_float(row[first + i]), nan) : -INFINITY;
+}
+
+template <typename T, int V> bool whole_rows(int64_t ld, int n_experts) {
+    const int bytes = V * (int)sizeof(T) < 16 ? V * (int)sizeof(T) : 16;
+    return n_experts % V == 0 && ld * (int64_t)sizeof(T) % bytes == 0;
 }
 
 // Scores in place of logits; 0 for what cannot be chosen.
 template <int V>
-__device__ __forceinline__ void scores_of(float (&x)[V], bool sigmoid) {
-    if (sigmoid) {
+__device__ __forceinline__ void scores_of(float (&x)[V], bool sigmoid_score) {
+    if (sigmoid_score) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = x[i] == -INFINITY ? 0.f : 1.f / (1.f + expf(-x[i]));
+        for (int i = 0; i < V; ++i) x[i] = sigmoid(x[i]);
         return;
     }
     float top = x[0];
@@ -80,118 +106,270 @@ __device__ __forceinline__ void scores_of(float (&x)[V], bool sigmoid) {
 #pragma unroll
     for (int i = 0; i < V; ++i) { x[i] = x[i] == -INFINITY ? 0.f : expf(x[i] - top); sum += x[i]; }
     sum = warp_sum(sum);
-    const float inv_safe = sum > 0.f ? sum : 1.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = x[i] / inv_safe;
-}
-
-// Best key of the warp and its lowest expert; removes it from its lane.
-template <int V>
-__device__ __forceinline__ unsigned take_best(unsigned (&key)[V], int lane, int lo, int hi, int *expert) {
-    unsigned best = 0;
-    int at = 0x7FFFFFFF;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = i * 32 + lane;
-        if (e >= lo && e < hi && key[i] > best) { best = key[i]; at = e; }
-    }
-    const unsigned top = __reduce_max_sync(kFull, best);
-    const unsigned who = __reduce_min_sync(kFull, best == top ? (unsigned)at : 0x7FFFFFFFu);
-    *expert = top ? (int)who : -1;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (top && i * 32 + lane == (int)who) key[i] = 0;
-    return top;
+    for (int i = 0; i < V; ++i) x[i] = sum > 0.f ? x[i] / sum : 0.f;
 }
 
 __device__ __forceinline__ float value_of(unsigned key) {
     return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
 
+// Best of a lane's keys in [lo, hi), the lowest index among equal ones.
+template <int V>
+__device__ __forceinline__ void lane_best(const unsigned (&key)[V], unsigned *best, int *at) {
+    *best = key[0];
+    *at = 0;
+#pragma unroll
+    for (int i = 1; i < V; ++i) if (key[i] > *best) { *best = key[i]; *at = i; }
+}
+
+// Key of the group's score that a lane's experts belong to, where every group is a power of two of
+// whole lanes: the two best of every lane, merged between its lanes.
+template <int V>
+__device__ __forceinline__ unsigned group_key(const unsigned (&key)[V], int lanes, int group_top) {
+    unsigned k1 = 0, k2 = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) { k2 = max(k2, min(k1, key[i])); k1 = max(k1, key[i]); }
+    for (int o = 1; o < lanes; o <<= 1) {
+        const unsigned o1 = __shfl_xor_sync(kFull, k1, o), o2 = __shfl_xor_sync(kFull, k2, o);
+        k2 = max(max(k2, o2), min(k1, o1));
+        k1 = max(k1, o1);
+    }
+    return group_top == 2 && k2 ? key_of(value_of(k1) + value_of(k2)) : k1;
+}
+
+// ... of group g for any other size; every lane gets it.
+template <int V>
+__device__ __forceinline__ unsigned group_key_any(const unsigned (&key)[V], int lane, int lo, int hi, int group_top) {
+    unsigned k1 = 0, k2 = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane * V + i;
+        const unsigned k = e >= lo && e < hi ? key[i] : 0u;
+        k2 = max(k2, min(k1, k));
+        k1 = max(k1, k);
+    }
+    const unsigned top = __reduce_max_sync(kFull, k1);
+    if (group_top < 2) return top;
+    const int owner = __ffs(__ballot_sync(kFull, k1 == top)) - 1;
+    const unsigned second = __reduce_max_sync(kFull, lane == owner ? k2 : k1);
+    return second ? key_of(value_of(top) + value_of(second)) : top;
+}
+
+// Which experts of the row are in the groups that are kept: keys of the others become 0.
+template <int V>
+__device__ __forceinline__ void keep_groups(unsigned (&key)[V], const RouterParams &p, int lane) {
+    const int lanes = p.group_size / V;
+    const bool even = lanes * V == p.group_size && (lanes & (lanes - 1)) == 0;
+    unsigned mine = 0;                               // lane g: key of group g's score
+    if (even) {
+        const unsigned own = group_key<V>(key, lanes, p.group_top);
+        mine = __shfl_sync(kFull, own, lane * lanes & 31);
+        if (lane >= p.n_groups) mine = 0;
+    } else {
+        for (int g = 0; g < p.n_groups; ++g) {
+            const unsigned k = group_key_any<V>(key, lane, g * p.group_size, (g + 1) * p.group_size, p.group_top);
+            if (lane == g) mine = k;
+        }
+    }
+    int before = 0;                                  // groups that rank before this lane's
+    for (int g = 0; g < p.n_groups; ++g) {
+        const unsigned other = __shfl_sync(kFull, mine, g);
+        before += other > mine || (other == mine && g < lane);
+    }
+    const unsigned kept = __ballot_sync(kFull, lane < p.n_groups && before < p.top_groups);
+    if (even) {
+        if (!((kept >> (lane / lanes & 31)) & 1)) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) key[i] = 0;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = lane * V + i;
+            if (e < p.n_experts && !((kept >> (e / p.group_size)) & 1)) key[i] = 0;
+        }
+    }
+}
+
 // One warp per row, V * 32 experts at most.
 template <typename T, int V>
+__device__ __forceinline__ void route_rows(const T *__restrict__ logits, int64_t first, int64_t last, int64_t ld, bool whole,
+                                           const float *__restrict__ bias, const RouterParams &p,
+                                           int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
+                                           int *cta_count, float (*scores)[V * 32], unsigned *__restrict__ status)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float b[V];
+    bool nan = false, inf = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane * V + i;
+        b[i] = bias && e < p.n_experts ? clean_logit(bias[e], &nan) : 0.f;
+        inf |= b[i] == -INFINITY;
+    }
+    for (int64_t n = first + warp; n < last; n += blockDim.x >> 5) {
+        float s[V];
+        unsigned key[V];
+        load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s, &nan);
+        unsigned off = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) off |= (s[i] == -INFINITY || (inf && b[i] == -INFINITY) ? 1u : 0u) << i;
+        scores_of<V>(s, p.sigmoid);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            key[i] = (off >> i) & 1 ? 0u : key_of(s[i] + b[i]);
+            scores[warp][lane * V + i] = s[i];
+        }
+        if (p.n_groups > 1) keep_groups<V>(key, p, lane);
+        int my_expert = -1;                          // lane j: slot j
+        unsigned best;
+        int at;
+        lane_best<V>(key, &best, &at);
+        for (int j = 0; j < p.top_k; ++j) {
+            const unsigned top = __reduce_max_sync(kFull, best);
+            if (top == 0) break;
+            const int owner = __ffs(__ballot_sync(kFull, best == top)) - 1;
+            const int e = __shfl_sync(kFull, lane * V + at, owner);
+            if (lane == j) my_expert = e;
+            if (lane == owner) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) if (i == at) key[i] = 0;
+                lane_best<V>(key, &best, &at);
+            }
+            __syncwarp();
+        }
+        const float my_score = my_expert >= 0 ? scores[warp][my_expert] : 0.f;
+        const float total = warp_sum(my_score) + kSumFloor;
+        if (lane < p.top_k) {
+            out_expert[n * p.top_k + lane] = my_expert;
+            out_weight[n * p.top_k + lane] = p.scale * (p.renormalise ? my_score / total : my_score);
+            if (cta_count && my_expert >= 0) atomicAdd(&cta_count[my_expert], 1);
+        }
+        __syncwarp();
+    }
+    if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+}
+
+template <typename T, int V>
 __global__ void __launch_bounds__(kRouteThreads)
-route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, const float *__restrict__ bias,
+route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bool whole, const float *__restrict__ bias,
                   RouterParams p, int rows_per_cta, int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
                   int *__restrict__ counts, unsigned *__restrict__ status)
 {
-    __shared__ int cta_count[GS_MAX_EXPERTS];
+    __shared__ int cta_count[V * 32];
+    __shared__ float scores[kRouteThreads / 32][V * 32];
     dependent_begin();
     for (int e = threadIdx.x; e < p.n_experts; e += kRouteThreads) cta_count[e] = 0;
     __syncthreads();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t first = (int64_t)blockIdx.x * rows_per_cta;
-    const int64_t last = min(first + rows_per_cta, n_tokens);
-    float b[V];
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = i * 32 + lane;
-        b[i] = bias && e < p.n_experts ? fminf(bias[e], kLargest) : 0.f;
-        if (b[i] != b[i]) { nan = true; b[i] = -INFINITY; }
-    }
-    for (int64_t n = first + warp; n < last; n += kRouteThreads / 32) {
-        float s[V];
-        unsigned key[V];
-        nan |= load_row<T, V>(logits + n * ld, p.n_experts, lane, s);
-        bool on[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) on[i] = s[i] != -INFINITY && b[i] != -INFINITY;
-        scores_of<V>(s, p.sigmoid);
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = on[i] ? key_of(s[i] + b[i]) : 0u;
-        if (p.n_groups > 1) {
-            unsigned mine = 0;                       // lane g: key of group g's score
-            for (int g = 0; g < p.n_groups; ++g) {
-                unsigned left[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) left[i] = key[i];
-                int at;
-                const int lo = g * p.group_size, hi = lo + p.group_size;
-                const unsigned k1 = take_best<V>(left, lane, lo, hi, &at);
-                unsigned score = k1;
-                if (p.group_top == 2 && k1) {
-                    const unsigned k2 = take_best<V>(left, lane, lo, hi, &at);
-                    if (k2) score = key_of(value_of(k1) + value_of(k2));
-                }
-                if (lane == g) mine = score;
-            }
-            int before = 0;                          // groups that rank before this lane's
-            for (int g = 0; g < p.n_groups; ++g) {
-                const unsigned other = __shfl_sync(kFull, mine, g);
-                before += other > mine || (other == mine && g < lane);
-            }
-            const unsigned kept = __ballot_sync(kFull, lane < p.n_groups && before < p.top_groups);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int e = i * 32 + lane;
-                if (e < p.n_experts && !((kept >> (e / p.group_size)) & 1)) key[i] = 0;
-            }
-        }
-        int my_expert = -1;                          // lane j: slot j
-        float my_score = 0.f;
-        for (int j = 0; j < p.top_k; ++j) {
-            int e;
-            take_best<V>(key, lane, 0, p.n_experts, &e);
-            float v = 0.f;
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (e == i * 32 + lane) v = s[i];
-            v = __shfl_sync(kFull, v, e & 31);
-            if (lane == j && e >= 0) { my_expert = e; my_score = v; }
-        }
-        const float total = warp_sum(my_score) + kSumFloor;
-        if (lane < p.top_k) {
-            const float w = p.renormalise ? p.scale * (my_score / total) : p.scale * my_score;
-            out_expert[n * p.top_k + lane] = my_expert;
-            out_weight[n * p.top_k + lane] = w;
-            if (counts && my_expert >= 0) atomicAdd(&cta_count[my_expert], 1);
-        }
-    }
-    if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    route_rows<T, V>(logits, first, min(first + rows_per_cta, n_tokens), ld, whole, bias, p, out_expert, out_weight,
+                     counts ? cta_count : nullptr, scores, status);
     if (!counts) return;
     __syncthreads();
     for (int e = threadIdx.x; e < p.n_experts; e += kRouteThreads)
         counts[e * kMaxRouteCtas + blockIdx.x] = cta_count[e];
+}
+
+// Few experts without groups: one thread per row, all of its scores in registers (E of them, a
+// multiple of four; those past the last expert are taken out of the choice).
+template <typename T, int E>
+__device__ __forceinline__ void load_token(const T *__restrict__ row, int n_experts, float (&x)[E], bool *nan) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = e < n_experts ? clean_logit(to_float(row[e]), nan) : -INFINITY;
+}
+
+template <int E>
+__device__ __forceinline__ void token_scores(float (&x)[E], bool sigmoid_score) {
+    if (sigmoid_score) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = sigmoid(x[e]);
+        return;
+    }
+    float top = x[0], sum = 0.f;
+#pragma unroll
+    for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) { x[e] = x[e] == -INFINITY ? 0.f : expf(x[e] - top); sum += x[e]; }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= inv;
+}
+
+// count: this thread's column of [experts][threads] counters in shared memory, or null
+template <typename T, int E>
+__device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n, const float *__restrict__ bias, const RouterParams &p,
+                                            int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
+                                            int *count, int stride, bool *nan)
+{
+    float s[E];
+    load_token<T, E>(row, p.n_experts, s, nan);
+    unsigned left = 0;                               // experts that may still be chosen
+#pragma unroll
+    for (int e = 0; e < E; ++e) left |= (s[e] != -INFINITY ? 1u : 0u) << e;
+    token_scores<E>(s, p.sigmoid);
+    float c[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        c[e] = s[e];
+        if (bias && e < p.n_experts) {
+            const float b = clean_logit(__ldg(bias + e), nan);
+            if (b == -INFINITY) left &= ~(1u << e); else c[e] += b;
+        }
+    }
+    float total = kSumFloor, q[GS_MAX_TOP_K];
+    int32_t *to = out_expert + n * p.top_k;
+#pragma unroll
+    for (int j = 0; j < GS_MAX_TOP_K; ++j) {
+        if (j >= p.top_k) break;
+        float best = 0.f, score = 0.f;
+        int at = -1;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (((left >> e) & 1) && (at < 0 || c[e] > best)) { best = c[e]; score = s[e]; at = e; }
+        if (at >= 0) {
+            left &= ~(1u << at);
+            if (count) count[at * stride] += 1;
+        }
+        to[j] = at;
+        q[j] = score;
+        total += score;
+    }
+#pragma unroll
+    for (int j = 0; j < GS_MAX_TOP_K; ++j) {
+        if (j >= p.top_k) break;
+        out_weight[n * p.top_k + j] = p.scale * (p.renormalise ? q[j] / total : q[j]);
+    }
+}
+
+template <typename T, int E>
+__global__ void __launch_bounds__(kRouteThreads)
+route_tokens_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, const float *__restrict__ bias,
+                    RouterParams p, int rows_per_cta, int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
+                    int *__restrict__ counts, unsigned *__restrict__ status)
+{
+    __shared__ int count[E * kRouteThreads];
+    dependent_begin();
+    int *mine = nullptr;
+    if (counts) {
+        mine = count + threadIdx.x;
+#pragma unroll
+        for (int e = 0; e < E; ++e) mine[e * kRouteThreads] = 0;
+    }
+    const int64_t first = (int64_t)blockIdx.x * rows_per_cta, last = min(first + rows_per_cta, n_tokens);
+    bool nan = false;
+    for (int64_t n = first + threadIdx.x; n < last; n += kRouteThreads)
+        route_token<T, E>(logits + n * ld, n, bias, p, out_expert, out_weight, mine, kRouteThreads, &nan);
+    if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    if (!counts) return;
+    __syncthreads();
+    for (int e = threadIdx.x >> 5; e < p.n_experts; e += kRouteThreads / 32) {
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < kRouteThreads / 32; ++i) sum += count[e * kRouteThreads + i * 32 + (threadIdx.x & 31)];
+        sum = __reduce_add_sync(kFull, sum);
+        if ((threadIdx.x & 31) == 0) counts[e * kMaxRouteCtas + blockIdx.x] = sum;
+    }
 }
 
 // Per expert (one warp each): counts per CTA become the rows before that CTA's, and their total.
@@ -217,42 +395,19 @@ route_prefix_kernel(int *__restrict__ counts, int n_experts, int n_ctas)
     if (lane == 0) counts[GS_MAX_EXPERTS * kMaxRouteCtas + e] = before;
 }
 
-// Places every slot of the CTA's tokens: each warp takes a stretch of them, first counts its
-// experts, then (knowing what the warps before it hold) hands out rows in order.
-__global__ void __launch_bounds__(kRouteThreads)
-route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_k, int slots_per_cta, int n_experts,
-                   const int *__restrict__ counts, int32_t *__restrict__ offsets, int32_t *__restrict__ row_token,
-                   int32_t *__restrict__ token_row)
+// Places the slots [cta_first, cta_last): each warp takes a stretch of them, first counts its
+// experts, then (knowing what the warps before it hold) hands out rows in order.  cnt: [warps]
+// [n_experts] counters in shared memory; base(e): first row of expert e for this CTA, called once
+// every warp has counted.
+template <typename Base>
+__device__ __forceinline__ void place_slots(const int32_t *expert, int64_t cta_first, int64_t cta_last, int top_k, int n_experts,
+                                            int *cnt, Base &&base, int32_t *__restrict__ row_token, int32_t *__restrict__ token_row)
 {
-    constexpr int kWarps = kRouteThreads / 32;
-    extern __shared__ int place_smem[];
-    int *cnt = place_smem;                           // [kWarps][n_experts]
-    int *start = place_smem + kWarps * n_experts;    // [n_experts + 1]
-    dependent_begin();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int *total = counts + GS_MAX_EXPERTS * kMaxRouteCtas;
-    for (int i = threadIdx.x; i < kWarps * n_experts; i += kRouteThreads) cnt[i] = 0;
-    if (warp == 0) {
-        int before = 0;
-        for (int base = 0; base < n_experts; base += 32) {
-            const int e = base + lane, own = e < n_experts ? total[e] : 0;
-            int sum = own;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int up = __shfl_up_sync(kFull, sum, o);
-                if (lane >= o) sum += up;
-            }
-            if (e < n_experts) start[e] = before + sum - own;
-            before += __shfl_sync(kFull, sum, 31);
-        }
-        if (lane == 0) start[n_experts] = before;
-    }
+    const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < warps * n_experts; i += blockDim.x) cnt[i] = 0;
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= n_experts; e += kRouteThreads) offsets[e] = start[e];
-    const int64_t cta_first = (int64_t)blockIdx.x * slots_per_cta, cta_last = min(cta_first + slots_per_cta, n_slots);
-    const int per_warp = ((slots_per_cta + kWarps - 1) / kWarps + 31) / 32 * 32;
-    const int64_t first = cta_first + (int64_t)warp * per_warp, last = min(first + per_warp, cta_last);
+    const int64_t per_warp = ((cta_last - cta_first + warps - 1) / warps + 31) / 32 * 32;
+    const int64_t first = min(cta_first + warp * per_warp, cta_last), last = min(first + per_warp, cta_last);
     int *mine = cnt + warp * n_experts;
     for (int64_t i = first + lane; i - lane < last; i += 32) {
         const int e = i < last ? expert[i] : -1;
@@ -261,10 +416,7 @@ route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_
         __syncwarp();
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < n_experts; e += kRouteThreads) {
-        int row = start[e] + counts[e * kMaxRouteCtas + blockIdx.x];
-        for (int w = 0; w < kWarps; ++w) { const int c = cnt[w * n_experts + e]; cnt[w * n_experts + e] = row; row += c; }
-    }
+    base(cnt, warps);
     __syncthreads();
     for (int64_t i = first + lane; i - lane < last; i += 32) {
         const int e = i < last ? expert[i] : -1;
@@ -279,10 +431,90 @@ route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_
             if (row >= 0) row_token[row] = (int)((unsigned)i / (unsigned)top_k);
         }
     }
+}
+
+// start[e] = sum of total(e') over e' < e, by one warp; start[n_experts] = all.
+template <typename Total>
+__device__ __forceinline__ void prefix_experts(int n_experts, int lane, int *start, Total &&total) {
+    int before = 0;
+    for (int base = 0; base < n_experts; base += 32) {
+        const int e = base + lane, own = e < n_experts ? total(e) : 0;
+        int sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(kFull, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (e < n_experts) start[e] = before + sum - own;
+        before += __shfl_sync(kFull, sum, 31);
+    }
+    if (lane == 0) start[n_experts] = before;
+}
+
+__global__ void __launch_bounds__(kRouteThreads)
+route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_k, int slots_per_cta, int n_experts,
+                   const int *__restrict__ counts, int32_t *__restrict__ offsets, int32_t *__restrict__ row_token,
+                   int32_t *__restrict__ token_row)
+{
+    extern __shared__ int place_smem[];
+    int *start = place_smem, *cnt = start + n_experts + 1;     // [n_experts + 1], [warps][n_experts]
+    dependent_begin();
+    const int *total = counts + GS_MAX_EXPERTS * kMaxRouteCtas;
+    if (threadIdx.x < 32) prefix_experts(n_experts, threadIdx.x, start, [&](int e) { return total[e]; });
+    const int64_t first = min((int64_t)blockIdx.x * slots_per_cta, n_slots), last = min(first + slots_per_cta, n_slots);
+    place_slots(expert, first, last, top_k, n_experts, cnt, [&](int *c, int warps) {
+        for (int e = threadIdx.x; e < n_experts; e += kRouteThreads) {
+            int row = start[e] + counts[e * kMaxRouteCtas + blockIdx.x];
+            for (int w = 0; w < warps; ++w) { const int own = c[w * n_experts + e]; c[w * n_experts + e] = row; row += own; }
+        }
+    }, row_token, token_row);
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= n_experts; e += kRouteThreads) offsets[e] = start[e];
     // rows that no slot took
     const int64_t step = (int64_t)gridDim.x * kRouteThreads;
     for (int64_t i = start[n_experts] + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; i < n_slots; i += step)
         row_token[i] = -1;
+}
+
+// Few tokens: choice and order in one launch of one CTA.
+constexpr int kSmallThreads = 512;
+template <typename T, int V, bool kTokens>
+__global__ void __launch_bounds__(kSmallThreads)
+route_small_kernel(const T *__restrict__ logits, int n_tokens, int64_t ld, bool whole, const float *__restrict__ bias,
+                   RouterParams p, int32_t *out_expert, float *__restrict__ out_weight, int32_t *__restrict__ offsets,
+                   int32_t *__restrict__ row_token, int32_t *__restrict__ token_row, unsigned *__restrict__ status)
+{
+    extern __shared__ int place_smem[];
+    int *start = place_smem, *cnt = start + p.n_experts + 1;   // scores of the rows before cnt is in use
+    dependent_begin();
+    if constexpr (kTokens) {
+        bool nan = false;
+        for (int n = threadIdx.x; n < n_tokens; n += kSmallThreads)
+            route_token<T, V>(logits + n * ld, n, bias, p, out_expert, out_weight, nullptr, 0, &nan);
+        if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    } else {
+        route_rows<T, V>(logits, 0, n_tokens, ld, whole, bias, p, out_expert, out_weight, nullptr,
+                         reinterpret_cast<float (*)[V * 32]>(cnt), status);
+    }
+    __syncthreads();
+    const int n_slots = n_tokens * p.top_k;
+    place_slots(out_expert, 0, n_slots, p.top_k, p.n_experts, cnt, [&](int *c, int warps) {
+        // rows of every expert: a warp's count becomes the rows of the warps before it, then the experts before it are added
+        for (int e = threadIdx.x; e < p.n_experts; e += kSmallThreads) {
+            int row = 0;
+            for (int w = 0; w < warps; ++w) { const int own = c[w * p.n_experts + e]; c[w * p.n_experts + e] = row; row += own; }
+            start[e] = row;
+        }
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            // (each lane reads its own totals before any of the batch is overwritten)
+            prefix_experts(p.n_experts, threadIdx.x, start, [&](int e) { return start[e]; });
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < warps * p.n_experts; i += kSmallThreads) c[i] += start[i % p.n_experts];
+    }, row_token, token_row);
+    for (int e = threadIdx.x; e <= p.n_experts; e += kSmallThreads) offsets[e] = start[e];
+    for (int i = start[p.n_experts] + threadIdx.x; i < n_slots; i += kSmallThreads) row_token[i] = -1;
 }
 
 // Gradient of the weights, one warp per row.  With q the chosen scores, t = sum q + 1e-20:
@@ -290,56 +522,125 @@ route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_
 //   sigmoid: dx = dq * s (1 - s);   softmax: dx = s * (dq - sum_j dq_j s_j)
 template <typename T, int V>
 __global__ void __launch_bounds__(kRouteThreads)
-route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, RouterParams p,
+route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bool whole, RouterParams p,
                            const int32_t *__restrict__ expert, const float *__restrict__ d_weight,
-                           T *__restrict__ d_logits, int64_t ld_d, unsigned *__restrict__ status)
+                           T *__restrict__ d_logits, int64_t ld_d, bool whole_d, unsigned *__restrict__ status)
 {
+    constexpr int kWarps = kRouteThreads / 32;
+    __shared__ __align__(16) float row_smem[kWarps][V * 32];   // a row's scores, then the gradients of those that were chosen
     dependent_begin();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float *mine = row_smem[warp];
     bool bad = false;
-    for (int64_t n = (int64_t)blockIdx.x * (kRouteThreads / 32) + warp; n < n_tokens; n += (int64_t)gridDim.x * (kRouteThreads / 32)) {
+    for (int64_t n = (int64_t)blockIdx.x * kWarps + warp; n < n_tokens; n += (int64_t)gridDim.x * kWarps) {
         float s[V];
-        bad |= load_row<T, V>(logits + n * ld, p.n_experts, lane, s);
-        scores_of<V>(s, p.sigmoid);
+        load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s, &bad);
         int e = lane < p.top_k ? expert[n * p.top_k + lane] : -1;
         if (e < -1 || e >= p.n_experts) { bad = true; e = -1; }
         const float dw = e >= 0 ? d_weight[n * p.top_k + lane] : 0.f;
-        float q = 0.f;                               // lane j: the score of slot j
-        for (int j = 0; j < p.top_k; ++j) {
-            const int ej = __shfl_sync(kFull, e, j);
-            float v = 0.f;
+        scores_of<V>(s, p.sigmoid);
 #pragma unroll
-            for (int i = 0; i < V; ++i) if (ej == i * 32 + lane) v = s[i];
-            v = __shfl_sync(kFull, v, ej & 31);
-            if (lane == j && ej >= 0) q = v;
-        }
+        for (int i = 0; i < V; ++i) mine[lane * V + i] = s[i];
+        __syncwarp();
+        const float q = e >= 0 ? mine[e] : 0.f;      // lane j: the score of slot j
+        __syncwarp();
         float dq = p.scale * dw;
         if (p.renormalise) {
-            const float t = warp_sum(q) + kSumFloor;
-            const float mean = warp_sum(dw * (q / t));
+            const float t = warp_sum(q) + kSumFloor, mean = warp_sum(dw * (q / t));
             dq = e >= 0 ? p.scale * ((dw - mean) / t) : 0.f;
-        }
-        float ds[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) ds[i] = 0.f;
-        for (int j = 0; j < p.top_k; ++j) {
-            const int ej = __shfl_sync(kFull, e, j);
-            const float v = __shfl_sync(kFull, dq, j);
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (ej == i * 32 + lane) ds[i] += v;
         }
         const float mean = p.sigmoid ? 0.f : warp_sum(dq * q);
 #pragma unroll
+        for (int i = 0; i < V; ++i) mine[lane * V + i] = 0.f;
+        __syncwarp();
+        if (e >= 0) atomicAdd(&mine[e], dq);         // (a row names an expert once)
+        __syncwarp();
+        float dx[V];
+#pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int k = i * 32 + lane;
-            const float dx = p.sigmoid ? ds[i] * s[i] * (1.f - s[i]) : s[i] * (ds[i] - mean);
-            if (k < p.n_experts) d_logits[n * ld_d + k] = from_float<T>(dx);
+            const float ds = mine[lane * V + i];
+            dx[i] = p.sigmoid ? ds * s[i] * (1.f - s[i]) : s[i] * (ds - mean);
+        }
+        __syncwarp();
+        T *out = d_logits + n * ld_d + lane * V;
+        if (whole_d) {
+            constexpr int kBytes = V * sizeof(T) < 16 ? V * sizeof(T) : 16, kEach = kBytes / sizeof(T);
+            using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, unsigned, unsigned short>>>;
+            if (lane * V < p.n_experts) {
+#pragma unroll
+                for (int w = 0; w < V / kEach; ++w) {
+                    Word word;
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) reinterpret_cast<T *>(&word)[i] = from_float<T>(dx[w * kEach + i]);
+                    reinterpret_cast<Word *>(out)[w] = word;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (lane * V + i < p.n_experts) out[i] = from_float<T>(dx[i]);
         }
     }
     if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
 }
 
-template <typename F> cudaError_t by_width(int n_experts, F &&f) {
+template <typename T, int E>
+__global__ void __launch_bounds__(kRouteThreads)
+route_tokens_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, RouterParams p,
+                             const int32_t *__restrict__ expert, const float *__restrict__ d_weight,
+                             T *__restrict__ d_logits, int64_t ld_d, unsigned *__restrict__ status)
+{
+    dependent_begin();
+    bool bad = false;
+    for (int64_t n = (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; n < n_tokens; n += (int64_t)gridDim.x * kRouteThreads) {
+        float s[E], ds[E];
+        load_token<T, E>(logits + n * ld, p.n_experts, s, &bad);
+        token_scores<E>(s, p.sigmoid);
+        unsigned chosen = 0;
+        float sum = kSumFloor, mean = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) ds[e] = 0.f;
+        for (int j = 0; j < p.top_k; ++j) {
+            const int at = expert[n * p.top_k + j];
+            if (at < -1 || at >= p.n_experts) { bad = true; continue; }
+            if (at < 0) continue;
+            const float dw = d_weight[n * p.top_k + j];
+#pragma unroll
+            for (int e = 0; e < E; ++e) if (e == at) { ds[e] += dw; sum += s[e]; }
+            chosen |= 1u << at;
+        }
+        if (p.renormalise) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) mean += ds[e] * (s[e] / sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) ds[e] = (chosen >> e) & 1 ? (ds[e] - mean) / sum : 0.f;
+        }
+        float across = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) { ds[e] *= p.scale; across += ds[e] * s[e]; }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float dx = p.sigmoid ? ds[e] * s[e] * (1.f - s[e]) : s[e] * (ds[e] - across);
+            if (e < p.n_experts) d_logits[n * ld_d + e] = from_float<T>(dx);
+        }
+    }
+    if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+}
+
+// One thread per row up to this many experts (without groups), one warp per row above and with groups.
+constexpr int kTokenExperts = 32;
+
+template <typename F> cudaError_t by_token_width(int n_experts, F &&f) {
+    switch ((n_experts + 3) / 4) {
+        case 1: return f(std::integral_constant<int, 4>());
+        case 2: return f(std::integral_constant<int, 8>());
+        case 3: return f(std::integral_constant<int, 12>());
+        case 4: return f(std::integral_constant<int, 16>());
+        case 5: case 6: return f(std::integral_constant<int, 24>());
+        default: return f(std::integral_constant<int, 32>());
+    }
+}
+
+template <typename F> cudaError_t by_row_width(int n_experts, F &&f) {
     if (n_experts <= 32) return f(std::integral_constant<int, 1>());
     if (n_experts <= 64) return f(std::integral_constant<int, 2>());
     if (n_experts <= 128) return f(std::integral_constant<int, 4>());
@@ -347,59 +648,97 @@ template <typename F> cudaError_t by_width(int n_experts, F &&f) {
     return f(std::integral_constant<int, 16>());
 }
 
-template <typename T>
-cudaError_t route_rows(gs_ctx *ctx, const ExpertRouteArgs &a, int n_ctas, int rows_per_cta, cudaStream_t st) {
-    int *counts = a.offsets ? operator_scratch(ctx).expert_counts : nullptr;
-    return by_width(a.r.n_experts, [&](auto v) {
-        LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
-        return launch_dependent(route_rows_kernel<T, decltype(v)::value>, dim3(n_ctas), dim3(kRouteThreads), 0, st,
-                                (const T *)a.logits, a.n_tokens, a.ld, a.bias, params_of(a.r), rows_per_cta,
-                                a.expert, a.weight, counts, ctx->s.status);
-    });
+int route_ctas(const gs_ctx *ctx) {
+    const int most = ctx->n_sm * 4;
+    return most < kMaxRouteCtas ? most : kMaxRouteCtas;
 }
 
-template <typename T>
-cudaError_t route_rows_backward(gs_ctx *ctx, const ExpertRouteGradArgs &a, cudaStream_t st) {
-    const int64_t want = (a.n_tokens + kRouteThreads / 32 - 1) / (kRouteThreads / 32);
-    const int n_ctas = (int)(want < 16 * ctx->n_sm ? want : 16 * ctx->n_sm);
-    return by_width(a.r.n_experts, [&](auto v) {
+template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a, cudaStream_t st) {
+    const RouterParams p = params_of(a.r);
+    const bool tokens = p.n_experts <= kTokenExperts && p.n_groups == 1;
+    const T *logits = (const T *)a.logits;
+    if (a.offsets && a.n_tokens <= (tokens ? 2 * kSmallThreads : kSmallThreads / 32 * 8)) {
+        const size_t counters = sizeof(int) * (kSmallThreads / 32) * (size_t)p.n_experts, lead = sizeof(int) * (p.n_experts + 1);
         LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
-        return launch_dependent(route_rows_backward_kernel<T, decltype(v)::value>, dim3(n_ctas), dim3(kRouteThreads), 0, st,
-                                (const T *)a.logits, a.n_tokens, a.ld, params_of(a.r), a.expert, a.d_weight,
-                                (T *)a.d_logits, a.ld_d, ctx->s.status);
+        if (tokens)
+            return by_token_width(p.n_experts, [&](auto v) {
+                return launch_dependent(route_small_kernel<T, decltype(v)::value, true>, dim3(1), dim3(kSmallThreads), lead + counters, st,
+                                        logits, (int)a.n_tokens, a.ld, false, a.bias, p, a.expert, a.weight, a.offsets, a.row_token,
+                                        a.token_row, ctx->s.status);
+            });
+        return by_row_width(p.n_experts, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            const size_t scores = sizeof(float) * (kSmallThreads / 32) * V * 32;
+            return launch_dependent(route_small_kernel<T, V, false>, dim3(1), dim3(kSmallThreads), lead + (counters > scores ? counters : scores), st,
+                                    logits, (int)a.n_tokens, a.ld, whole_rows<T, V>(a.ld, p.n_experts), a.bias, p, a.expert, a.weight,
+                                    a.offsets, a.row_token, a.token_row, ctx->s.status);
+        });
+    }
+    const int at_once = tokens ? kRouteThreads : kRouteThreads / 32;         // rows of a CTA
+    const int64_t want = (a.n_tokens + at_once - 1) / at_once;
+    const int n_ctas = want < route_ctas(ctx) ? (int)want : route_ctas(ctx);
+    const int rows_per_cta = (int)(((a.n_tokens + n_ctas - 1) / n_ctas + at_once - 1) / at_once * at_once);
+    int *counts = a.offsets ? operator_scratch(ctx).expert_counts : nullptr;
+    cudaError_t e;
+    {
+        LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
+        if (tokens)
+            e = by_token_width(p.n_experts, [&](auto v) {
+                return launch_dependent(route_tokens_kernel<T, decltype(v)::value>, dim3(n_ctas), dim3(kRouteThreads), 0, st,
+                                        logits, a.n_tokens, a.ld, a.bias, p, rows_per_cta, a.expert, a.weight, counts, ctx->s.status);
+            });
+        else
+            e = by_row_width(p.n_experts, [&](auto v) {
+                constexpr int V = decltype(v)::value;
+                return launch_dependent(route_rows_kernel<T, V>, dim3(n_ctas), dim3(kRouteThreads), 0, st, logits, a.n_tokens, a.ld,
+                                        whole_rows<T, V>(a.ld, p.n_experts), a.bias, p, rows_per_cta, a.expert, a.weight, counts, ctx->s.status);
+            });
+    }
+    if (e != cudaSuccess || !counts) return e;
+    const int warps = kRouteThreads / 32;
+    {
+        LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
+        e = launch_dependent(route_prefix_kernel, dim3((p.n_experts + warps - 1) / warps), dim3(kRouteThreads), 0, st,
+                             counts, p.n_experts, n_ctas);
+    }
+    if (e != cudaSuccess) return e;
+    const size_t smem = sizeof(int) * ((size_t)warps * p.n_experts + p.n_experts + 1);
+    LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
+    return launch_dependent(route_place_kernel, dim3(n_ctas), dim3(kRouteThreads), smem, st, (const int32_t *)a.expert,
+                            a.n_tokens * p.top_k, p.top_k, rows_per_cta * p.top_k, p.n_experts,
+                            (const int *)counts, a.offsets, a.row_token, a.token_row);
+}
+
+template <typename T> cudaError_t route_backward_as(gs_ctx *ctx, const ExpertRouteGradArgs &a, cudaStream_t st) {
+    const RouterParams p = params_of(a.r);
+    const bool tokens = p.n_experts <= kTokenExperts;
+    const int at_once = tokens ? kRouteThreads : kRouteThreads / 32;
+    const int64_t want = (a.n_tokens + at_once - 1) / at_once, most = (int64_t)ctx->n_sm * 16;
+    const dim3 grid((unsigned)(want < most ? want : most));
+    LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
+    if (tokens)
+        return by_token_width(p.n_experts, [&](auto v) {
+            return launch_dependent(route_tokens_backward_kernel<T, decltype(v)::value>, grid, dim3(kRouteThreads), 0, st,
+                                    (const T *)a.logits, a.n_tokens, a.ld, p, a.expert, a.d_weight, (T *)a.d_logits, a.ld_d, ctx->s.status);
+        });
+    return by_row_width(p.n_experts, [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        return launch_dependent(route_rows_backward_kernel<T, V>, grid, dim3(kRouteThreads), 0, st, (const T *)a.logits, a.n_tokens, a.ld,
+                                whole_rows<T, V>(a.ld, p.n_experts), p, a.expert, a.d_weight, (T *)a.d_logits, a.ld_d,
+                                whole_rows<T, V>(a.ld_d, p.n_experts), ctx->s.status);
     });
 }
 
 }  // namespace
 
 cudaError_t launch_expert_route(gs_ctx *ctx, const ExpertRouteArgs &a, cudaStream_t st) {
-    const int warps = kRouteThreads / 32;
-    int64_t want = (a.n_tokens + warps - 1) / warps;
-    const int most = ctx->n_sm * 4 < kMaxRouteCtas ? ctx->n_sm * 4 : kMaxRouteCtas;
-    const int n_ctas = want < 1 ? 1 : want < most ? (int)want : most;
-    const int rows_per_cta = (int)((a.n_tokens + n_ctas - 1) / n_ctas);
-    cudaError_t e = a.dtype == GS_F32 ? route_rows<float>(ctx, a, n_ctas, rows_per_cta, st)
-                  : a.dtype == GS_BF16 ? route_rows<__nv_bfloat16>(ctx, a, n_ctas, rows_per_cta, st)
-                                       : route_rows<__half>(ctx, a, n_ctas, rows_per_cta, st);
-    if (e != cudaSuccess || !a.offsets) return e;
-    int *counts = operator_scratch(ctx).expert_counts;
-    {
-        LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
-        e = launch_dependent(route_prefix_kernel, dim3((a.r.n_experts + warps - 1) / warps), dim3(kRouteThreads), 0, st,
-                             counts, a.r.n_experts, n_ctas);
-    }
-    if (e != cudaSuccess) return e;
-    const size_t smem = sizeof(int) * ((size_t)warps * a.r.n_experts + a.r.n_experts + 1);
-    LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
-    return launch_dependent(route_place_kernel, dim3(n_ctas), dim3(kRouteThreads), smem, st, a.expert,
-                            a.n_tokens * a.r.top_k, a.r.top_k, rows_per_cta * a.r.top_k, a.r.n_experts,
-                            counts, a.offsets, a.row_token, a.token_row);
+    return a.dtype == GS_F32 ? route_as<float>(ctx, a, st)
+         : a.dtype == GS_BF16 ? route_as<__nv_bfloat16>(ctx, a, st) : route_as<__half>(ctx, a, st);
 }
 
 cudaError_t launch_expert_route_backward(gs_ctx *ctx, const ExpertRouteGradArgs &a, cudaStream_t st) {
-    return a.dtype == GS_F32 ? route_rows_backward<float>(ctx, a, st)
-         : a.dtype == GS_BF16 ? route_rows_backward<__nv_bfloat16>(ctx, a, st)
-                              : route_rows_backward<__half>(ctx, a, st);
+    return a.dtype == GS_F32 ? route_backward_as<float>(ctx, a, st)
+         : a.dtype == GS_BF16 ? route_backward_as<__nv_bfloat16>(ctx, a, st) : route_backward_as<__half>(ctx, a, st);
 }
 
 }  // namespace gs
