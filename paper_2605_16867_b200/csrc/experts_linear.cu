@@ -125,14 +125,16 @@ template <int kN> struct RowsShape {
     static constexpr uint32_t kBBytes = kN / 2 * 128;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = kN == 256 ? 6 : kN == 128 ? 8 : kN == 64 ? 9 : 10;
-    static constexpr int kStoreBytes = 4 * 2048;             // per warp: 32 requests x 32 features
+    static constexpr int kStoreWarps = kN >= 64 ? 8 : 4;
+    static constexpr int kStoreBytes = kStoreWarps * 2048;   // per warp: 32 requests x 32 features
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + sizeof(Barriers) + (3 * GS_MAX_EXPERTS + 4) * sizeof(int);
     static constexpr int kTmem = 2 * kN < 32 ? 32 : 2 * kN;
+    static constexpr int threads(bool gather) { return 32 * (2 + kStoreWarps + (gather ? kGatherWarps - 1 : 0)); }
 };
 
 // kDx: the weights' tile has its features contiguous (the contraction runs over their rows).
 template <typename T, bool kDx, int kN, bool kGather>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGather ? 160 + 32 * kGatherWarps : 192, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(RowsShape<kN>::threads(kGather), 1)
 rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const RowsArgs p)
 {
     using S = RowsShape<kN>;
@@ -146,7 +148,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     volatile int *failed = &bars->failed;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    setup_pair(bars, S::kStages, 4, warp, lane);
+    setup_pair(bars, S::kStages, S::kStoreWarps, warp, lane);
     if (warp == kWarpMma) tmem_alloc<S::kTmem>(smem_u32(&bars->tmem));
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 0) scan_row_tiles(p.offsets, p.n_experts, p.n_rows, kN, tile_start, row_start, row_end, lane);
@@ -160,8 +162,8 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     const int64_t n_tiles = (int64_t)tile_start[p.n_experts] * m_tiles;
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
-    if (warp == kWarpProducer || warp >= 6) {
-        const int helper = warp == kWarpProducer ? 0 : warp - 5;     // kGatherWarps warps share out the gathered rows
+    if (warp == kWarpProducer || warp >= 2 + S::kStoreWarps) {
+        const int helper = warp == kWarpProducer ? 0 : warp - (1 + S::kStoreWarps);     // kGatherWarps warps share out the gathered rows
         if (threadIdx.x == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
         Ring ring;
         int e = 0;
@@ -223,20 +225,37 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             }
         }
     } else {
-        const int quarter = warp & 3;                         // the lanes of tensor memory that this warp reads
-        T *mine = reinterpret_cast<T *>(store + quarter * 2048);
+        // lanes of tensor memory that this warp reads, and its columns
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        constexpr int kCols = kN / (S::kStoreWarps / 4);
+        T *mine = reinterpret_cast<T *>(store + (warp - 2) * 2048);
         int e = 0, use = 0;
         bool bad = false;
         for (int64_t t = pair; t < n_tiles; t += n_pairs, ++use) {
             const int rt = (int)(t / m_tiles), f0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM + quarter * 32;
             while (tile_start[e + 1] <= rt) ++e;
-            const int r0 = row_start[e] + (rt - tile_start[e]) * kN, r1 = min(r0 + kN, row_end[e]);
+            const int r0 = row_start[e] + (rt - tile_start[e]) * kN + half * kCols, r1 = min(r0 + kCols, row_end[e]);
             const float add = p.bias && f0 + lane < p.features ? p.bias[(int64_t)e * p.features + f0 + lane] : 0.f;
+            // a lane's four pieces of a block of 32 requests: eight features of request i * 8 + lane / 4 each
+            const int f = f0 + lane % 4 * 8, width = min(8, p.features - f);
+            uint4 keep[4];                                    // the mask's values there, asked for a block ahead
+            const auto ask = [&](int c) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + c + i * 8 + lane / 4;
+                    keep[i] = make_uint4(0, 0, 0, 0);
+                    if (r < r1 && width == 8) {
+                        const int64_t token = p.row_token ? safe_token(p.row_token[r], p.n_tokens, &bad) : r;
+                        keep[i] = *reinterpret_cast<const uint4 *>((const T *)p.mask + token * p.ld_mask + f);
+                    }
+                }
+            };
+            if (kDx && p.mask) ask(0);
             if (!warp_wait(smem_u32(&bars->sums_full[use & 1]), (use >> 1) & 1, failed)) break;
             fence_after();
-            const uint32_t sums = tmem + (use & 1) * kN + ((uint32_t)(quarter * 32) << 16);
+            const uint32_t sums = tmem + (use & 1) * kN + half * kCols + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
-            for (int c = 0; c < kN; c += 32) {
+            for (int c = 0; c < kCols; c += 32) {
                 if (r0 + c >= r1 || f0 >= p.features) break;
                 float v[32];
                 tmem_load32(sums + c, v);
@@ -247,32 +266,36 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                     mine[i * 32 + lane] = from_float<T>(z);
                 }
                 __syncwarp();
+                uint4 q[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = i * 32 + lane, r = r0 + c + at / 4, f = f0 + at % 4 * 8;
-                    if (r >= r1 || f >= p.features) continue;
-                    uint4 q = *reinterpret_cast<const uint4 *>(mine + at * 8);
-                    T *z = reinterpret_cast<T *>(&q);
-                    const int n = min(8, p.features - f);
+                    q[i] = *reinterpret_cast<const uint4 *>(mine + (i * 32 + lane) * 8);
                     if (kDx && p.mask) {
-                        const int token = p.row_token ? safe_token(p.row_token[r], p.n_tokens, &bad) : r;
-                        const T *x = (const T *)p.mask + token * p.ld_mask + f;
-                        if (n == 8) {
-                            const uint4 xq = *reinterpret_cast<const uint4 *>(x);
-                            const T *xs = reinterpret_cast<const T *>(&xq);
+                        T *z = reinterpret_cast<T *>(&q[i]);
+                        const T *x = reinterpret_cast<const T *>(&keep[i]);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) if (!(to_float(xs[j]) > 0.f)) z[j] = from_float<T>(0.f);
-                        } else {
-                            for (int j = 0; j < n; ++j) if (!(to_float(x[j]) > 0.f)) z[j] = from_float<T>(0.f);
-                        }
+                        for (int j = 0; j < 8; ++j) if (width == 8 && !(to_float(x[j]) > 0.f)) z[j] = from_float<T>(0.f);
                     }
+                }
+                if (kDx && p.mask) ask(c + 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + c + i * 8 + lane / 4;
+                    if (r >= r1 || width <= 0) continue;
                     T *out = (T *)p.out + r * p.ld_out + f;
-                    if (n == 8) *reinterpret_cast<uint4 *>(out) = q;
-                    else for (int j = 0; j < n; ++j) out[j] = z[j];
+                    if (width == 8) {
+                        *reinterpret_cast<uint4 *>(out) = q[i];
+                        continue;
+                    }
+                    const T *z = reinterpret_cast<const T *>(&q[i]);
+                    const T *x = nullptr;
+                    if (kDx && p.mask) x = (const T *)p.mask + (p.row_token ? safe_token(p.row_token[r], p.n_tokens, &bad) : r) * p.ld_mask + f;
+                    for (int j = 0; j < width; ++j) out[j] = x && !(to_float(x[j]) > 0.f) ? from_float<T>(0.f) : z[j];
                 }
                 __syncwarp();
             }
             fence_before();
+            __syncwarp();
             if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
         }
         if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
@@ -306,9 +329,14 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 // first in features.
 
 constexpr int kMinPiece = 32;                   // steps of 64 rows; an expert is not cut finer
-constexpr int kPiecesPerPair = 2;
+constexpr int kPiecesPerPair = 1;
 constexpr int kChain = 8;                       // steps
-constexpr int kWeightsStoreWarps = 8, kWarpClear = 2 + kWeightsStoreWarps, kWeightsThreads = 32 * (kWarpClear + 1);
+// Warps: 0 copies, 1 issues the matrix instructions, 2 clears; the last eight store.  With gathered
+// rows 3 to 7 issue the gathers, and registers move from the first eight warps to the storing ones
+// (which hold 128 sums a thread): 256 * 56 + 256 * 184 of the 512 * 128 that the block starts with.
+constexpr int kWeightsStoreWarps = 8, kWarpClear = 2, kWarpGather = 3, kGatherWarpsDw = 5;
+constexpr int kFewRegs = 56, kManyRegs = 184;
+__host__ __device__ constexpr int weights_threads(bool gather) { return gather ? 512 : 384; }
 
 struct WeightsArgs {
     const int32_t *offsets, *row_token;
@@ -319,83 +347,119 @@ struct WeightsArgs {
     unsigned *status;
 };
 
+// How every expert's rows are cut, in shared memory.
+struct Pieces {
+    int row_start[GS_MAX_EXPERTS], row_end[GS_MAX_EXPERTS], count[GS_MAX_EXPERTS];
+    int slot_start[GS_MAX_EXPERTS];             // partial sums of the cut experts before it
+    int at[GS_MAX_EXPERTS];                     // experts, those with the longest pieces first
+    int unit_start[GS_MAX_EXPERTS + 1];         // units (tiles of pieces) of the experts before the i-th of them
+};
+
 template <int kN> struct WeightsShape {
     static constexpr uint32_t kBBytes = kN / 2 * 128;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = kN == 256 ? 6 : 8;
     static constexpr int kStoreBytes = kWeightsStoreWarps * 2048;      // per warp: 32 x 16 floats
     static constexpr int kOnesBytes = 2048;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + kOnesBytes + sizeof(Barriers) + (5 * GS_MAX_EXPERTS + 8) * sizeof(int);
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + kOnesBytes + sizeof(Barriers) + sizeof(Pieces);
     static constexpr int kTmem = 2 * kN;
     static constexpr int kPartial = kTileM * kN + kTileM;    // floats of one piece: sums, then db
 };
 
-struct Pieces {
-    int *unit_start, *slot_start, *row_start, *row_end, *count;
-};
+__device__ __forceinline__ int steps_of(const Pieces &s, int e) { return (s.row_end[e] - s.row_start[e] + kDepth - 1) / kDepth; }
+__device__ __forceinline__ int piece_steps(const Pieces &s, int e) { return (steps_of(s, e) + s.count[e] - 1) / s.count[e]; }
 
-// Cuts every expert's rows into pieces; units: tiles of pieces, slots: those whose sums are partial.
+__device__ __forceinline__ int warp_prefix(int v, int lane, int *total) {
+    int sum = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(kFull, sum, o);
+        if (lane >= o) sum += up;
+    }
+    *total = __shfl_sync(kFull, sum, 31);
+    return sum - v;
+}
+
+// By one warp: rows, pieces and slots of every expert.
 __device__ __forceinline__ void scan_pieces(const int32_t *__restrict__ offsets, int n_experts, int n_rows, int tiles, int n_pairs,
-                                            const Pieces &s, int lane) {
+                                            Pieces &s, int lane) {
     int64_t steps = 0;
     int end = 0;
     for (int base = 0; base < n_experts; base += 32) {
         const int2 r = ascending_rows(offsets, base + lane, n_experts, n_rows, lane, &end);
+        if (base + lane < n_experts) { s.row_start[base + lane] = r.x; s.row_end[base + lane] = r.y; }
         steps += (r.y - r.x + kDepth - 1) / kDepth;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) steps += __shfl_xor_sync(kFull, steps, o);
     const int64_t share = (steps * tiles + n_pairs * kPiecesPerPair - 1) / (n_pairs * kPiecesPerPair);
     const int most = (int)(share < kMinPiece ? kMinPiece : share);
-    int units = 0, slots = 0;
-    end = 0;
+    int slots = 0;
     for (int base = 0; base < n_experts; base += 32) {
-        const int e = base + lane;
-        const int2 r = ascending_rows(offsets, e, n_experts, n_rows, lane, &end);
-        const int own_steps = (r.y - r.x + kDepth - 1) / kDepth;
-        const int pieces = e < n_experts ? max((own_steps + most - 1) / most, 1) : 0;
-        int u = pieces * tiles, v = pieces > 1 ? pieces * tiles : 0;
-        const int own_u = u, own_v = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up_u = __shfl_up_sync(kFull, u, o), up_v = __shfl_up_sync(kFull, v, o);
-            if (lane >= o) { u += up_u; v += up_v; }
-        }
-        if (e < n_experts) {
-            s.unit_start[e] = units + u - own_u;
-            s.slot_start[e] = slots + v - own_v;
-            s.row_start[e] = r.x;
-            s.row_end[e] = r.y;
-            s.count[e] = pieces;
-        }
-        units += __shfl_sync(kFull, u, 31);
-        slots += __shfl_sync(kFull, v, 31);
+        const int e = base + lane, pieces = e < n_experts ? max((steps_of(s, e) + most - 1) / most, 1) : 0;
+        int all;
+        const int before = warp_prefix(pieces > 1 ? pieces * tiles : 0, lane, &all);
+        if (e < n_experts) { s.count[e] = pieces; s.slot_start[e] = slots + before; }
+        slots += all;
     }
-    if (lane == 0) s.unit_start[n_experts] = units;
+}
+
+// By the whole block: the order of the units, those with the longest pieces first.  Dealt out to the
+// pairs forth and back, every pair gets nearly the same number of steps.
+__device__ __forceinline__ void order_units(int n_experts, int tiles, Pieces &s) {
+    for (int e = threadIdx.x; e < n_experts; e += blockDim.x) {
+        const int own = piece_steps(s, e);
+        int rank = 0;
+        for (int o = 0; o < n_experts; ++o) {
+            const int other = piece_steps(s, o);
+            rank += other > own || (other == own && o < e);
+        }
+        s.at[rank] = e;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        int units = 0;
+        for (int base = 0; base < n_experts; base += 32) {
+            const int i = base + (int)threadIdx.x;
+            int all;
+            const int before = warp_prefix(i < n_experts ? s.count[s.at[i]] * tiles : 0, threadIdx.x, &all);
+            if (i < n_experts) s.unit_start[i] = units + before;
+            units += all;
+        }
+        if (threadIdx.x == 0) s.unit_start[n_experts] = units;
+    }
 }
 
 // One unit of work: a tile of one piece of an expert's rows.
 struct Unit {
-    int e, piece, m0, n0, first, last, steps, slot;
+    int e, m0, n0, first, last, steps, slot;
 };
-__device__ __forceinline__ Unit unit_of(const Pieces &s, int u, int e, int n_tiles_n, int tiles, int kn) {
-    Unit w;
-    const int in_e = u - s.unit_start[e], tile = in_e % tiles;
-    w.e = e;
-    w.piece = in_e / tiles;
-    w.m0 = tile / n_tiles_n * kTileM;
-    w.n0 = tile % n_tiles_n * kn;
-    const int rows = s.row_end[e] - s.row_start[e], steps = (rows + kDepth - 1) / kDepth, pieces = s.count[e];
-    const int per = (steps + pieces - 1) / pieces, s0 = min(w.piece * per, steps), s1 = min(s0 + per, steps);
-    w.steps = s1 - s0;
-    w.first = s.row_start[e] + s0 * kDepth;
-    w.last = min(s.row_start[e] + s1 * kDepth, s.row_end[e]);
-    w.slot = pieces > 1 ? s.slot_start[e] + in_e : -1;
-    return w;
-}
+// The pair's units in turn.
+struct Units {
+    const Pieces &s;
+    const int pair, n_pairs, n_units, tiles, tiles_n, kn;
+    int round = 0, i = 0;
+    __device__ __forceinline__ bool next(Unit *w) {
+        const int64_t u64 = (int64_t)round * n_pairs + ((round & 1) ? n_pairs - 1 - pair : pair);
+        ++round;
+        if (u64 >= n_units) return false;
+        const int u = (int)u64;
+        while (s.unit_start[i + 1] <= u) ++i;
+        const int e = s.at[i], in_e = u - s.unit_start[i], tile = in_e % tiles, piece = in_e / tiles;
+        w->e = e;
+        w->m0 = tile / tiles_n * kTileM;
+        w->n0 = tile % tiles_n * kn;
+        const int steps = steps_of(s, e), per = piece_steps(s, e), s0 = min(piece * per, steps), s1 = min(s0 + per, steps);
+        w->steps = s1 - s0;
+        w->first = s.row_start[e] + s0 * kDepth;
+        w->last = min(s.row_start[e] + s1 * kDepth, s.row_end[e]);
+        w->slot = s.count[e] > 1 ? s.slot_start[e] + in_e : -1;
+        return true;
+    }
+};
 
 template <typename T, int kN, bool kGather>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWeightsThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(weights_threads(kGather), 1)
 weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant__ CUtensorMap map_x, const WeightsArgs p)
 {
     using S = WeightsShape<kN>;
@@ -403,12 +467,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
     unsigned char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char *ones = smem + S::kStages * S::kStageBytes, *store = ones + S::kOnesBytes;
     Barriers *bars = reinterpret_cast<Barriers *>(store + S::kStoreBytes);
-    Pieces s;
-    s.unit_start = reinterpret_cast<int *>(bars + 1);
-    s.slot_start = s.unit_start + GS_MAX_EXPERTS + 1;
-    s.row_start = s.slot_start + GS_MAX_EXPERTS;
-    s.row_end = s.row_start + GS_MAX_EXPERTS;
-    s.count = s.row_end + GS_MAX_EXPERTS;
+    Pieces &s = *reinterpret_cast<Pieces *>(bars + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     volatile int *failed = &bars->failed;
@@ -424,27 +483,35 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 0) scan_pieces(p.offsets, p.n_experts, p.n_rows, tiles, n_pairs, s, lane);
+    __syncthreads();
+    order_units(p.n_experts, tiles, s);
     fence_before();
     __syncthreads();
     cluster_sync();
     fence_after();
 
     const uint32_t tmem = bars->tmem;
-    const int n_units = s.unit_start[p.n_experts];
+    Units units = {s, pair, n_pairs, s.unit_start[p.n_experts], tiles, tiles_n, kN};
+    Unit w;
+    constexpr int kFirstStore = weights_threads(kGather) / 32 - kWeightsStoreWarps;
+    if constexpr (kGather) {
+        if (warp < kFirstStore) fewer_registers<kFewRegs>();
+    }
 
-    if (warp == kWarpProducer) {
-        if (lane == 0) { prefetch_map(&map_dz); prefetch_map(&map_x); }
+    if (warp == kWarpProducer || (kGather && warp >= kWarpGather && warp < kFirstStore)) {
+        const int helper = warp - kWarpGather;               // of kGatherWarpsDw; negative: the copying warp
+        if (threadIdx.x == 0) { prefetch_map(&map_dz); prefetch_map(&map_x); }
+        // sixteen groups of four rows, kN / 128 columns of boxes, dealt out to the warps and their lanes
+        const int job = lane * kGatherWarpsDw + helper, group = job % 16, box = job / 16;
+        const bool gathers = kGather && helper >= 0 && job < 16 * (kN / 128);
         Ring ring;
-        int e = 0;
         bool bad = false, ok = true;
-        for (int u = pair; u < n_units && ok; u += n_pairs) {
-            while (s.unit_start[e + 1] <= u) ++e;
-            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+        while (ok && units.next(&w)) {
             const int a0 = w.m0 + (int)rank * kHalfM, b0 = w.n0 + (int)rank * (kN / 2);
             int token[4];
-            if (kGather && w.steps > 0) {
+            if (gathers && w.steps > 0) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(w.first + lane % 16 * 4 + i, w.last - 1)];
+                for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(w.first + group * 4 + i, w.last - 1)];
             }
             for (int k = 0; k < w.steps; ++k) {
                 const int r = w.first + k * kDepth;
@@ -453,7 +520,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
                 const uint32_t a = smem_u32(smem + ring.stage * S::kStageBytes), b = a + kABytes;
                 // (a step that has to be cleared lands on this CTA's own barrier; an address of the CTA itself is one of the cluster too)
                 const uint32_t full = tail ? smem_u32(&bars->landed[ring.stage]) : in_leader(smem_u32(&bars->full[ring.stage]));
-                if (lane == 0) {
+                if (warp == kWarpProducer && lane == 0) {
                     bar_expect(full, S::kStageBytes);
                     copy_2d(&map_dz, a, full, a0, r);
                     copy_2d(&map_dz, a + kABytes / 2, full, a0 + 64, r);
@@ -461,19 +528,17 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
 #pragma unroll
                         for (int i = 0; i < kN / 128; ++i) copy_2d(&map_x, b + i * 8192, full, b0 + i * 64, r);
                 }
-                if (kGather) {
+                if (gathers) {
                     int t[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) t[i] = safe_token(token[i], p.n_tokens, &bad);
-                    if (k + 1 < w.steps) {
+                    copy_rows4(&map_x, b + box * 8192 + group * 512, full, b0 + box * 64, t[0], t[1], t[2], t[3]);
+                    if (k + 1 < w.steps) {                    // the next step's rows
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(r + kDepth + lane % 16 * 4 + i, w.last - 1)];
+                        for (int i = 0; i < 4; ++i) token[i] = p.row_token[min(r + kDepth + group * 4 + i, w.last - 1)];
                     }
-                    __syncwarp();
-                    // sixteen groups of four rows, kN / 128 columns of boxes, dealt out to the lanes
-                    for (int i = lane / 16; i < kN / 128; i += 2)
-                        copy_rows4(&map_x, b + i * 8192 + lane % 16 * 512, full, b0 + i * 64, t[0], t[1], t[2], t[3]);
                 }
+                __syncwarp();
                 ring.next(S::kStages);
             }
         }
@@ -484,12 +549,9 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
             constexpr uint32_t kInstrOnes = instruction(kBf16<T>, true, true, kTileM, 32);
             const uint64_t d_ones = operand(smem_u32(ones), 16);
             Ring ring;
-            int use = 0, e = 0;
+            int use = 0;
             bool ok = true;
-            for (int u = pair; u < n_units && ok; u += n_pairs) {
-                while (s.unit_start[e + 1] <= u) ++e;
-                const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
-                if (w.steps == 0) continue;
+            while (ok && units.next(&w)) {
                 const bool with_db = p.db && w.n0 == 0;
                 for (int k0 = 0; k0 < w.steps && ok; k0 += kChain) {
                     const uint32_t sums = tmem + (use & 1) * kN, other = tmem + (~use & 1) * kN;
@@ -522,12 +584,9 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
         }
     } else if (warp == kWarpClear) {
         Ring ring;
-        int e = 0;
         unsigned rounds = 0;                                 // bit s: parity of stage s's next landing
         bool ok = true;
-        for (int u = pair; u < n_units && ok; u += n_pairs) {
-            while (s.unit_start[e + 1] <= u) ++e;
-            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+        while (ok && units.next(&w)) {
             for (int k = 0; k < w.steps; ++k) {
                 const int left = w.last - (w.first + k * kDepth);
                 if (left < kDepth) {
@@ -545,16 +604,15 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
                 ring.next(S::kStages);
             }
         }
-    } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;       // lanes of tensor memory, columns of the tile
+    } else if (warp >= kFirstStore) {
+        if constexpr (kGather) more_registers<kManyRegs>();
+        const int quarter = warp & 3, half = (warp - kFirstStore) >> 2;       // lanes of tensor memory, columns of the tile
         constexpr int kCols = kN / 2;
-        float *mine = reinterpret_cast<float *>(store + (warp - 2) * 2048);
+        float *mine = reinterpret_cast<float *>(store + (warp - kFirstStore) * 2048);
         const uint32_t sums = tmem + ((uint32_t)(quarter * 32) << 16);
-        int use = 0, e = 0;
+        int use = 0;
         bool ok = true;
-        for (int u = pair; u < n_units && ok; u += n_pairs) {
-            while (s.unit_start[e + 1] <= u) ++e;
-            const Unit w = unit_of(s, u, e, tiles_n, tiles, kN);
+        while (ok && units.next(&w)) {
             const int row = (int)rank * kHalfM + quarter * 32, o0 = w.m0 + row;      // this warp's rows in the tile and in dW
             const bool with_db = p.db && w.n0 == 0;
             float v[kCols], bias = 0.f;
@@ -641,9 +699,8 @@ __global__ void __launch_bounds__(256)
 weights_sum_kernel(const WeightsArgs p, int n_pairs)
 {
     using S = WeightsShape<kN>;
-    __shared__ int tables[5 * GS_MAX_EXPERTS + 1];
+    __shared__ Pieces s;
     dependent_begin();
-    Pieces s = {tables, tables + GS_MAX_EXPERTS + 1, tables + 2 * GS_MAX_EXPERTS + 1, tables + 3 * GS_MAX_EXPERTS + 1, tables + 4 * GS_MAX_EXPERTS + 1};
     const int tiles_n = (p.n_in + kN - 1) / kN, tiles = tiles_n * ((p.n_out + kTileM - 1) / kTileM);
     if (threadIdx.x < 32) scan_pieces(p.offsets, p.n_experts, p.n_rows, tiles, n_pairs, s, threadIdx.x);
     __syncthreads();
@@ -660,6 +717,7 @@ weights_sum_kernel(const WeightsArgs p, int n_pairs)
                 const int row = part * 32 + i / (kN / 4), col4 = i % (kN / 4), o = m0 + row, col = n0 + col4 * 4;
                 if (o >= p.n_out || col >= p.n_in) continue;
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
                 for (int piece = 0; piece < s.count[e]; ++piece) {
                     const float4 q = *reinterpret_cast<const float4 *>(base + (int64_t)piece * tiles * S::kPartial + ((int64_t)col4 * kTileM + row) * 4);
                     sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
@@ -725,7 +783,7 @@ cudaError_t launch_rows(gs_ctx *ctx, const CUtensorMap &map_w, const CUtensorMap
     const int64_t tiles = (p.n_rows / kN + p.n_experts) * (int64_t)((p.features + kTileM - 1) / kTileM);
     const int pairs = (int)(tiles < pairs_of(ctx) ? tiles : pairs_of(ctx));
     LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(kGather ? 160 + 32 * kGatherWarps : 192), RowsShape<kN>::kSmem, st, map_w, map_x, p);
+    return launch_dependent(rows_kernel<T, kDx, kN, kGather>, dim3(2 * pairs), dim3(RowsShape<kN>::threads(kGather)), RowsShape<kN>::kSmem, st, map_w, map_x, p);
 }
 
 template <typename T> cudaError_t forward_as(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
@@ -769,12 +827,14 @@ template <typename T, int kN> cudaError_t dw_as(gs_ctx *ctx, const ExpertLinearA
     cudaError_t e;
     {
         LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-        e = a.row_token ? launch_dependent(weights_kernel<T, kN, true>, dim3(2 * pairs), dim3(kWeightsThreads), WeightsShape<kN>::kSmem, st, map_dz, map_x, p)
-                        : launch_dependent(weights_kernel<T, kN, false>, dim3(2 * pairs), dim3(kWeightsThreads), WeightsShape<kN>::kSmem, st, map_dz, map_x, p);
+        e = a.row_token ? launch_dependent(weights_kernel<T, kN, true>, dim3(2 * pairs), dim3(weights_threads(true)), WeightsShape<kN>::kSmem, st, map_dz, map_x, p)
+                        : launch_dependent(weights_kernel<T, kN, false>, dim3(2 * pairs), dim3(weights_threads(false)), WeightsShape<kN>::kSmem, st, map_dz, map_x, p);
     }
     if (e != cudaSuccess || expert_linear_workspace(ctx, a.n_experts, a.n_rows, a.in, a.out) == 0) return e;
+    // (not as a programmatic dependent: its CTAs would gather on the SMs whose pairs end first and stay
+    // there; 16,384 requests of 1024 to 512: 113 instead of 69 us for both launches)
     LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
-    return launch_dependent(weights_sum_kernel<kN>, dim3(4 * ctx->n_sm), dim3(256), 0, st, p, pairs);
+    return launch_after(weights_sum_kernel<kN>, dim3(4 * ctx->n_sm), dim3(256), 0, st, p, pairs);
 }
 
 template <typename T> cudaError_t dw_by_tile(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
@@ -788,8 +848,12 @@ template <typename T, int kN> cudaError_t configure_rows() {
     return e;
 }
 
+// The storing warps of the gathering kernel wait for registers that the others give back: there have to be enough.
 template <typename T, int kN> cudaError_t configure_weights() {
-    cudaError_t e = cudaFuncSetAttribute(weights_kernel<T, kN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WeightsShape<kN>::kSmem);
+    cudaFuncAttributes f;
+    cudaError_t e = cudaFuncGetAttributes(&f, weights_kernel<T, kN, true>);
+    if (e == cudaSuccess && f.numRegs * weights_threads(true) < 256 * (kFewRegs + kManyRegs)) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_kernel<T, kN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WeightsShape<kN>::kSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(weights_kernel<T, kN, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)WeightsShape<kN>::kSmem);
     return e;
 }

@@ -259,7 +259,7 @@ route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bo
 {
     __shared__ int cta_count[V * 32];
     __shared__ float scores[kRouteThreads / 32][V * 32];
-    dependent_begin();
+    dependent_wait();
     for (int e = threadIdx.x; e < p.n_experts; e += kRouteThreads) cta_count[e] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * rows_per_cta;
@@ -269,6 +269,7 @@ route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bo
     __syncthreads();
     for (int e = threadIdx.x; e < p.n_experts; e += kRouteThreads)
         counts[e * kMaxRouteCtas + blockIdx.x] = cta_count[e];
+    dependent_end();
 }
 
 // Few experts without groups: one thread per row, all of its scores in registers (E of them, a
@@ -349,7 +350,7 @@ route_tokens_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, 
                     int *__restrict__ counts, unsigned *__restrict__ status)
 {
     __shared__ int count[E * kRouteThreads];
-    dependent_begin();
+    dependent_wait();
     int *mine = nullptr;
     if (counts) {
         mine = count + threadIdx.x;
@@ -370,13 +371,14 @@ route_tokens_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, 
         sum = __reduce_add_sync(kFull, sum);
         if ((threadIdx.x & 31) == 0) counts[e * kMaxRouteCtas + blockIdx.x] = sum;
     }
+    dependent_end();
 }
 
 // Per expert (one warp each): counts per CTA become the rows before that CTA's, and their total.
 __global__ void __launch_bounds__(kRouteThreads)
 route_prefix_kernel(int *__restrict__ counts, int n_experts, int n_ctas)
 {
-    dependent_begin();
+    dependent_wait();
     const int e = blockIdx.x * (kRouteThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (e >= n_experts) return;
     int *c = counts + e * kMaxRouteCtas, before = 0;
@@ -393,6 +395,7 @@ route_prefix_kernel(int *__restrict__ counts, int n_experts, int n_ctas)
         before += __shfl_sync(kFull, sum, 31);
     }
     if (lane == 0) counts[GS_MAX_EXPERTS * kMaxRouteCtas + e] = before;
+    dependent_end();
 }
 
 // Places the slots [cta_first, cta_last): each warp takes a stretch of them, first counts its
@@ -458,7 +461,7 @@ route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_
 {
     extern __shared__ int place_smem[];
     int *start = place_smem, *cnt = start + n_experts + 1;     // [n_experts + 1], [warps][n_experts]
-    dependent_begin();
+    dependent_wait();
     const int *total = counts + GS_MAX_EXPERTS * kMaxRouteCtas;
     if (threadIdx.x < 32) prefix_experts(n_experts, threadIdx.x, start, [&](int e) { return total[e]; });
     const int64_t first = min((int64_t)blockIdx.x * slots_per_cta, n_slots), last = min(first + slots_per_cta, n_slots);
@@ -486,7 +489,7 @@ route_small_kernel(const T *__restrict__ logits, int n_tokens, int64_t ld, bool 
 {
     extern __shared__ int place_smem[];
     int *start = place_smem, *cnt = start + p.n_experts + 1;   // scores of the rows before cnt is in use
-    dependent_begin();
+    dependent_wait();
     if constexpr (kTokens) {
         bool nan = false;
         for (int n = threadIdx.x; n < n_tokens; n += kSmallThreads)
@@ -528,7 +531,7 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
 {
     constexpr int kWarps = kRouteThreads / 32;
     __shared__ __align__(16) float row_smem[kWarps][V * 32];   // a row's scores, then the gradients of those that were chosen
-    dependent_begin();
+    dependent_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float *mine = row_smem[warp];
     bool bad = false;
@@ -589,7 +592,7 @@ route_tokens_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int
                              const int32_t *__restrict__ expert, const float *__restrict__ d_weight,
                              T *__restrict__ d_logits, int64_t ld_d, unsigned *__restrict__ status)
 {
-    dependent_begin();
+    dependent_wait();
     bool bad = false;
     for (int64_t n = (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; n < n_tokens; n += (int64_t)gridDim.x * kRouteThreads) {
         float s[E], ds[E];

@@ -38,7 +38,23 @@ __device__ __forceinline__ void dependent_begin() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+// The same in two parts, for kernels of several CTAs per SM: CTAs of the next kernel that are set
+// up early gather on the SMs that have room first, and stay there.  So the next kernel is let in at
+// the end.
+__device__ __forceinline__ void dependent_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependent_end() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+
+// Launches a kernel once the one before it has ended (no programmatic dependence).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
 
 struct ExpertRouteArgs {
     const void *logits;

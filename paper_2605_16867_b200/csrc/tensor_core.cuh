@@ -98,6 +98,10 @@ __device__ __forceinline__ void copy_rows4(const CUtensorMap *m, uint32_t dst, u
 // Generic writes to shared memory become visible to copies and matrix instructions.
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ---- registers: a warpgroup gives some back, another takes them ----
+template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+
 // ---- tensor memory ----
 template <int kCols> __device__ __forceinline__ void tmem_alloc(uint32_t smem_slot) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_slot), "n"(kCols) : "memory");
