@@ -5,6 +5,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -16,8 +18,7 @@ DEBUG_LIB_PATH = os.path.join(_PKG, "libgoodserve_debug.so")    # the checking b
 SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu", "operators_api.cu", "experts_route.cu",
            "experts_linear.cu", "experts_combine.cu", "clip.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--shared",
-              "-cudart", "shared")
+              "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-cudart", "shared")
 
 
 def _nvcc() -> str:
@@ -46,11 +47,18 @@ def build_library(force: bool = False, verbose: bool = False, extra_flags=(), co
         extra_flags = (*extra_flags, "-DGS_COUNT_EVALS")
     elif checking:
         extra_flags = (*extra_flags, "-DGS_DEBUG")
-    cmd = [_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", path + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), file=sys.stderr)
-    subprocess.run(cmd, check=True)
+    # one compiler process per source file, side by side, then one link
+    with tempfile.TemporaryDirectory(prefix="goodserve_build_") as objects:
+        def compile_one(source: str) -> str:
+            obj = os.path.join(objects, source + ".o")
+            cmd = [_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj]
+            if verbose:
+                print(" ".join(cmd), file=sys.stderr)
+            subprocess.run(cmd, check=True)
+            return obj
+        with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as workers:
+            built = list(workers.map(compile_one, SOURCES))
+        subprocess.run([_nvcc(), *NVCC_FLAGS, "--shared", *built, "-o", path + ".tmp"], check=True)
     os.replace(path + ".tmp", path)
     return path
 

@@ -114,13 +114,33 @@ __device__ __forceinline__ float value_of(unsigned key) {
     return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-// Best of a lane's keys in [lo, hi), the lowest index among equal ones.
-template <int V>
-__device__ __forceinline__ void lane_best(const unsigned (&key)[V], unsigned *best, int *at) {
-    *best = key[0];
-    *at = 0;
+// A lane's keys in descending order, equal ones by index: an odd-even merge sort, its network laid
+// out at compile time (stages P = 1, 2, 4, ...; distances K = P, P / 2, ..., 1).
+template <int V, int P, int K>
+__device__ __forceinline__ void sort_step(unsigned (&key)[V], int (&at)[V]) {
+    if constexpr (P < V) {
 #pragma unroll
-    for (int i = 1; i < V; ++i) if (key[i] > *best) { *best = key[i]; *at = i; }
+        for (int lo = 0; lo < V - K; ++lo) {
+            const int hi = lo + K, j = K % P;
+            if (lo >= j && (lo - j) % (2 * K) < K && lo / (2 * P) == hi / (2 * P)) {
+                const bool swap = key[hi] > key[lo] || (key[hi] == key[lo] && at[hi] < at[lo]);
+                const unsigned k0 = key[lo], k1 = key[hi];
+                const int a0 = at[lo], a1 = at[hi];
+                key[lo] = swap ? k1 : k0;
+                key[hi] = swap ? k0 : k1;
+                at[lo] = swap ? a1 : a0;
+                at[hi] = swap ? a0 : a1;
+            }
+        }
+        if constexpr (K > 1) sort_step<V, P, K / 2>(key, at);
+        else sort_step<V, 2 * P, 2 * P>(key, at);
+    }
+}
+template <int V>
+__device__ __forceinline__ void sort_lane(unsigned (&key)[V], int (&at)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) at[i] = i;
+    sort_step<V, 1, 1>(key, at);
 }
 
 // Key of the group's score that a lane's experts belong to, where every group is a power of two of
@@ -222,23 +242,21 @@ __device__ __forceinline__ void route_rows(const T *__restrict__ logits, int64_t
             scores[warp][lane * V + i] = s[i];
         }
         if (p.n_groups > 1) keep_groups<V>(key, p, lane);
-        int my_expert = -1;                          // lane j: slot j
-        unsigned best;
-        int at;
-        lane_best<V>(key, &best, &at);
+        // every round takes the best head of the lanes' sorted lists
+        int my_expert = -1, order[V];                // lane j: slot j
+        sort_lane<V>(key, order);
         for (int j = 0; j < p.top_k; ++j) {
-            const unsigned top = __reduce_max_sync(kFull, best);
+            const unsigned top = __reduce_max_sync(kFull, key[0]);
             if (top == 0) break;
-            const int owner = __ffs(__ballot_sync(kFull, best == top)) - 1;
-            const int e = __shfl_sync(kFull, lane * V + at, owner);
+            const int owner = __ffs(__ballot_sync(kFull, key[0] == top)) - 1;
+            const int e = __shfl_sync(kFull, lane * V + order[0], owner);
             if (lane == j) my_expert = e;
-            if (lane == owner) {
+            const bool pop = lane == owner;
 #pragma unroll
-                for (int i = 0; i < V; ++i) if (i == at) key[i] = 0;
-                lane_best<V>(key, &best, &at);
-            }
-            __syncwarp();
+            for (int i = 0; i + 1 < V; ++i) { key[i] = pop ? key[i + 1] : key[i]; order[i] = pop ? order[i + 1] : order[i]; }
+            key[V - 1] = pop ? 0u : key[V - 1];
         }
+        __syncwarp();
         const float my_score = my_expert >= 0 ? scores[warp][my_expert] : 0.f;
         const float total = warp_sum(my_score) + kSumFloor;
         if (lane < p.top_k) {
@@ -272,12 +290,22 @@ route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bo
     dependent_end();
 }
 
-// Few experts without groups: one thread per row, all of its scores in registers (E of them, a
-// multiple of four; those past the last expert are taken out of the choice).
+// Few experts without groups: one thread per row, all of its scores in registers (E of them, the
+// experts or a few more; those past the last are taken out of the choice).
 template <typename T, int E>
 __device__ __forceinline__ void load_token(const T *__restrict__ row, int n_experts, float (&x)[E], bool *nan) {
+    bool any = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = e < n_experts ? clean_logit(to_float(row[e]), nan) : -INFINITY;
+    for (int e = 0; e < E; ++e) {
+        const float v = e < n_experts ? to_float(row[e]) : -INFINITY;
+        any |= v != v;
+        x[e] = fminf(v, kLargest);
+    }
+    if (any) {
+        *nan = true;
+#pragma unroll
+        for (int e = 0; e < E; ++e) if (e < n_experts && to_float(row[e]) != to_float(row[e])) x[e] = -INFINITY;
+    }
 }
 
 template <int E>
@@ -290,60 +318,60 @@ __device__ __forceinline__ void token_scores(float (&x)[E], bool sigmoid_score) 
     float top = x[0], sum = 0.f;
 #pragma unroll
     for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
+    top = fmaxf(top, -kLargest);                     // (a row with nothing left: every exponential is 0)
 #pragma unroll
-    for (int e = 0; e < E; ++e) { x[e] = x[e] == -INFINITY ? 0.f : expf(x[e] - top); sum += x[e]; }
+    for (int e = 0; e < E; ++e) { x[e] = expf(x[e] - top); sum += x[e]; }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= inv;
 }
 
 // count: this thread's column of [experts][threads] counters in shared memory, or null
-template <typename T, int E>
+template <typename T, int E, bool kBias>
 __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n, const float *__restrict__ bias, const RouterParams &p,
                                             int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
                                             int *count, int stride, bool *nan)
 {
-    float s[E];
+    float s[E], c[E];                                // score; choice score, -infinity where it cannot be chosen
     load_token<T, E>(row, p.n_experts, s, nan);
-    unsigned left = 0;                               // experts that may still be chosen
+    unsigned off = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) left |= (s[e] != -INFINITY ? 1u : 0u) << e;
+    for (int e = 0; e < E; ++e) off |= (s[e] == -INFINITY ? 1u : 0u) << e;
     token_scores<E>(s, p.sigmoid);
-    float c[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         c[e] = s[e];
-        if (bias && e < p.n_experts) {
-            const float b = clean_logit(__ldg(bias + e), nan);
-            if (b == -INFINITY) left &= ~(1u << e); else c[e] += b;
-        }
+        if (kBias && e < p.n_experts) c[e] += clean_logit(__ldg(bias + e), nan);
+        if ((off >> e) & 1) c[e] = -INFINITY;
     }
-    float total = kSumFloor, q[GS_MAX_TOP_K];
-    int32_t *to = out_expert + n * p.top_k;
-#pragma unroll
-    for (int j = 0; j < GS_MAX_TOP_K; ++j) {
-        if (j >= p.top_k) break;
-        float best = 0.f, score = 0.f;
+    int32_t *experts = out_expert + n * p.top_k;
+    float *weights = out_weight + n * p.top_k;
+    float total = kSumFloor;
+    // (weights are written unscaled and read back for the scaling: top_k is small, and so is the cache line)
+    float q0 = 0.f, q1 = 0.f;
+    for (int j = 0; j < p.top_k; ++j) {
+        float best = -INFINITY, score = 0.f;
         int at = -1;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (((left >> e) & 1) && (at < 0 || c[e] > best)) { best = c[e]; score = s[e]; at = e; }
+            if (c[e] > best) { best = c[e]; at = e; if (kBias) score = s[e]; }
         if (at >= 0) {
-            left &= ~(1u << at);
+            if (!kBias) score = best;
             if (count) count[at * stride] += 1;
-        }
-        to[j] = at;
-        q[j] = score;
-        total += score;
-    }
 #pragma unroll
-    for (int j = 0; j < GS_MAX_TOP_K; ++j) {
-        if (j >= p.top_k) break;
-        out_weight[n * p.top_k + j] = p.scale * (p.renormalise ? q[j] / total : q[j]);
+            for (int e = 0; e < E; ++e) if (e == at) c[e] = -INFINITY;
+        }
+        experts[j] = at;
+        total += score;
+        if (j == 0) q0 = score; else if (j == 1) q1 = score; else weights[j] = score;
     }
+    const float f = p.scale;
+    weights[0] = f * (p.renormalise ? q0 / total : q0);
+    if (p.top_k > 1) weights[1] = f * (p.renormalise ? q1 / total : q1);
+    for (int j = 2; j < p.top_k; ++j) weights[j] = f * (p.renormalise ? weights[j] / total : weights[j]);
 }
 
-template <typename T, int E>
+template <typename T, int E, bool kBias>
 __global__ void __launch_bounds__(kRouteThreads)
 route_tokens_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, const float *__restrict__ bias,
                     RouterParams p, int rows_per_cta, int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
@@ -360,7 +388,7 @@ route_tokens_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, 
     const int64_t first = (int64_t)blockIdx.x * rows_per_cta, last = min(first + rows_per_cta, n_tokens);
     bool nan = false;
     for (int64_t n = first + threadIdx.x; n < last; n += kRouteThreads)
-        route_token<T, E>(logits + n * ld, n, bias, p, out_expert, out_weight, mine, kRouteThreads, &nan);
+        route_token<T, E, kBias>(logits + n * ld, n, bias, p, out_expert, out_weight, mine, kRouteThreads, &nan);
     if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
     if (!counts) return;
     __syncthreads();
@@ -412,26 +440,38 @@ __device__ __forceinline__ void place_slots(const int32_t *expert, int64_t cta_f
     const int64_t per_warp = ((cta_last - cta_first + warps - 1) / warps + 31) / 32 * 32;
     const int64_t first = min(cta_first + warp * per_warp, cta_last), last = min(first + per_warp, cta_last);
     int *mine = cnt + warp * n_experts;
-    for (int64_t i = first + lane; i - lane < last; i += 32) {
-        const int e = i < last ? expert[i] : -1;
-        const unsigned same = __match_any_sync(kFull, e);
-        if (e >= 0 && __ffs(same) - 1 == lane) mine[e] += __popc(same);
-        __syncwarp();
+    constexpr int kAhead = 4;                        // slots of a lane asked for at once
+    for (int64_t i0 = first; i0 < last; i0 += 32 * kAhead) {
+        int e[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) e[k] = i0 + k * 32 + lane < last ? expert[i0 + k * 32 + lane] : -1;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const unsigned same = __match_any_sync(kFull, e[k]);
+            if (e[k] >= 0 && __ffs(same) - 1 == lane) mine[e[k]] += __popc(same);
+            __syncwarp();
+        }
     }
     __syncthreads();
     base(cnt, warps);
     __syncthreads();
-    for (int64_t i = first + lane; i - lane < last; i += 32) {
-        const int e = i < last ? expert[i] : -1;
-        const unsigned same = __match_any_sync(kFull, e);
-        int row = -1;
-        if (e >= 0) row = mine[e] + __popc(same & ((1u << lane) - 1));
-        __syncwarp();
-        if (e >= 0 && __ffs(same) - 1 == lane) mine[e] += __popc(same);
-        __syncwarp();
-        if (i < last) {
-            token_row[i] = row;
-            if (row >= 0) row_token[row] = (int)((unsigned)i / (unsigned)top_k);
+    for (int64_t i0 = first; i0 < last; i0 += 32 * kAhead) {
+        int e[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) e[k] = i0 + k * 32 + lane < last ? expert[i0 + k * 32 + lane] : -1;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = i0 + k * 32 + lane;
+            const unsigned same = __match_any_sync(kFull, e[k]);
+            int row = -1;
+            if (e[k] >= 0) row = mine[e[k]] + __popc(same & ((1u << lane) - 1));
+            __syncwarp();
+            if (e[k] >= 0 && __ffs(same) - 1 == lane) mine[e[k]] += __popc(same);
+            __syncwarp();
+            if (i < last) {
+                token_row[i] = row;
+                if (row >= 0) row_token[row] = (int)((unsigned)i / (unsigned)top_k);
+            }
         }
     }
 }
@@ -493,7 +533,8 @@ route_small_kernel(const T *__restrict__ logits, int n_tokens, int64_t ld, bool 
     if constexpr (kTokens) {
         bool nan = false;
         for (int n = threadIdx.x; n < n_tokens; n += kSmallThreads)
-            route_token<T, V>(logits + n * ld, n, bias, p, out_expert, out_weight, nullptr, 0, &nan);
+            if (bias) route_token<T, V, true>(logits + n * ld, n, bias, p, out_expert, out_weight, nullptr, 0, &nan);
+            else route_token<T, V, false>(logits + n * ld, n, bias, p, out_expert, out_weight, nullptr, 0, &nan);
         if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
     } else {
         route_rows<T, V>(logits, 0, n_tokens, ld, whole, bias, p, out_expert, out_weight, nullptr,
@@ -633,12 +674,14 @@ route_tokens_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int
 constexpr int kTokenExperts = 32;
 
 template <typename F> cudaError_t by_token_width(int n_experts, F &&f) {
-    switch ((n_experts + 3) / 4) {
-        case 1: return f(std::integral_constant<int, 4>());
-        case 2: return f(std::integral_constant<int, 8>());
-        case 3: return f(std::integral_constant<int, 12>());
-        case 4: return f(std::integral_constant<int, 16>());
-        case 5: case 6: return f(std::integral_constant<int, 24>());
+    switch (n_experts) {
+        case 1: case 2: case 3: case 4: return f(std::integral_constant<int, 4>());
+        case 5: case 6: return f(std::integral_constant<int, 6>());
+        case 7: case 8: return f(std::integral_constant<int, 8>());
+        case 9: case 10: return f(std::integral_constant<int, 10>());
+        case 11: case 12: return f(std::integral_constant<int, 12>());
+        case 13: case 14: case 15: case 16: return f(std::integral_constant<int, 16>());
+        case 17: case 18: case 19: case 20: case 21: case 22: case 23: case 24: return f(std::integral_constant<int, 24>());
         default: return f(std::integral_constant<int, 32>());
     }
 }
@@ -687,8 +730,9 @@ template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a
         LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
         if (tokens)
             e = by_token_width(p.n_experts, [&](auto v) {
-                return launch_dependent(route_tokens_kernel<T, decltype(v)::value>, dim3(n_ctas), dim3(kRouteThreads), 0, st,
-                                        logits, a.n_tokens, a.ld, a.bias, p, rows_per_cta, a.expert, a.weight, counts, ctx->s.status);
+                constexpr int E = decltype(v)::value;
+                return launch_dependent(a.bias ? route_tokens_kernel<T, E, true> : route_tokens_kernel<T, E, false>, dim3(n_ctas), dim3(kRouteThreads),
+                                        0, st, logits, a.n_tokens, a.ld, a.bias, p, rows_per_cta, a.expert, a.weight, counts, ctx->s.status);
             });
         else
             e = by_row_width(p.n_experts, [&](auto v) {
