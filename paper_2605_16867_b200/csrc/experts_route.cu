@@ -56,33 +56,52 @@ __device__ __forceinline__ float clean_logit(float v, bool *nan) {
     return fminf(v, kLargest);
 }
 
-// 1 / (1 + exp(-x)); the reciprocal is the approximate one (1 ulp).  0 at -infinity.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+// 2^y by the special function unit (2^-22 relative).  exp(x) = 2^(x log2 e): rounding the exponent
+// costs |x| * 2^-24, so a score of e^-10 is good to some 2^-20; the larger ones, which are chosen, to 2^-22.
+// (The library's exponential takes four times the instructions, and instructions bound these kernels.)
+__device__ __forceinline__ float exp2_fast(float y) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 
-// A row's logits, experts lane * V .. lane * V + V - 1; -infinity where there is none to choose.
+// 1 / (1 + exp(-x)); the reciprocal is the approximate one (1 ulp).  0 at -infinity.
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + exp2_fast(-kLog2e * x)); }
+
+// A row's logits, experts lane * V .. lane * V + V - 1; -infinity where there is none.
 // `whole`: rows start so aligned, and experts divide so evenly, that a lane's can be read at once.
+// True if one of them is infinite or not a number (or there is none): the caller then cleans them.
 template <typename T, int V>
-__device__ __forceinline__ void load_row(const T *__restrict__ row, int n_experts, int lane, bool whole, float (&x)[V], bool *nan) {
+__device__ __forceinline__ bool load_row(const T *__restrict__ row, int n_experts, int lane, bool whole, float (&x)[V]) {
     const int first = lane * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = -INFINITY;
     if (whole) {
         constexpr int kBytes = V * sizeof(T) < 16 ? V * sizeof(T) : 16, kEach = kBytes / sizeof(T);
         using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, unsigned, unsigned short>>>;
+        if (first < n_experts) {
 #pragma unroll
-        for (int w = 0; w < V / kEach; ++w) {
-            if (first < n_experts) {
-                const Word q = reinterpret_cast<const Word *>(row + first)[w];
+            for (int w = 0; w < V / kEach; ++w) {
+                const Word q = __ldg(reinterpret_cast<const Word *>(row + first) + w);
                 const T *t = reinterpret_cast<const T *>(&q);
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = clean_logit(to_float(t[i]), nan);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = -INFINITY;
+                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = to_float(t[i]);
             }
         }
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = first + i < n_experts ? clean_logit(to_float(row[first + i]), nan) : -INFINITY;
+        for (int i = 0; i < V; ++i) if (first + i < n_experts) x[i] = to_float(row[first + i]);
+    }
+    float odd = 0.f;                                 // 0 * x is not a number for either
+#pragma unroll
+    for (int i = 0; i < V; ++i) odd = fmaf(x[i], 0.f, odd);
+    return odd != odd;
+}
+
+template <int V> __device__ __forceinline__ void clean_row(float (&x)[V], bool *nan) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = clean_logit(x[i], nan);
 }
 
 template <typename T, int V> bool whole_rows(int64_t ld, int n_experts) {
@@ -101,13 +120,14 @@ __device__ __forceinline__ void scores_of(float (&x)[V], bool sigmoid_score) {
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) top = fmaxf(top, x[i]);
-    top = warp_max(top);
+    top = fmaxf(warp_max(top), -kLargest);           // (nothing left: every exponential is 0)
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) { x[i] = x[i] == -INFINITY ? 0.f : expf(x[i] - top); sum += x[i]; }
+    for (int i = 0; i < V; ++i) { x[i] = exp2_fast((x[i] - top) * kLog2e); sum += x[i]; }
     sum = warp_sum(sum);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = sum > 0.f ? x[i] / sum : 0.f;
+    for (int i = 0; i < V; ++i) x[i] *= inv;
 }
 
 __device__ __forceinline__ float value_of(unsigned key) {
@@ -176,13 +196,12 @@ __device__ __forceinline__ unsigned group_key_any(const unsigned (&key)[V], int 
     return second ? key_of(value_of(top) + value_of(second)) : top;
 }
 
-// Which experts of the row are in the groups that are kept: keys of the others become 0.
+// The groups that are kept, as a mask.  `lanes`: lanes of a group if all groups are the same power of
+// two of whole lanes, else 0.
 template <int V>
-__device__ __forceinline__ void keep_groups(unsigned (&key)[V], const RouterParams &p, int lane) {
-    const int lanes = p.group_size / V;
-    const bool even = lanes * V == p.group_size && (lanes & (lanes - 1)) == 0;
+__device__ __forceinline__ unsigned kept_groups(const unsigned (&key)[V], const RouterParams &p, int lanes, int lane) {
     unsigned mine = 0;                               // lane g: key of group g's score
-    if (even) {
+    if (lanes) {
         const unsigned own = group_key<V>(key, lanes, p.group_top);
         mine = __shfl_sync(kFull, own, lane * lanes & 31);
         if (lane >= p.n_groups) mine = 0;
@@ -197,71 +216,110 @@ __device__ __forceinline__ void keep_groups(unsigned (&key)[V], const RouterPara
         const unsigned other = __shfl_sync(kFull, mine, g);
         before += other > mine || (other == mine && g < lane);
     }
-    const unsigned kept = __ballot_sync(kFull, lane < p.n_groups && before < p.top_groups);
-    if (even) {
-        if (!((kept >> (lane / lanes & 31)) & 1)) {
+    return __ballot_sync(kFull, lane < p.n_groups && before < p.top_groups);
+}
+
+// The top_k best keys of the warp, slot j's expert in lane j (-1: none left).  first: the expert of a
+// lane's key 0; experts ascend with lanes.  Every round takes the best head of the lanes' sorted lists.
+template <int V>
+__device__ __forceinline__ int best_experts(unsigned (&key)[V], int first, int top_k, int lane) {
+    int mine = -1, at[V];
+    sort_lane<V>(key, at);
 #pragma unroll
-            for (int i = 0; i < V; ++i) key[i] = 0;
-        }
-    } else {
+    for (int i = 0; i < V; ++i) at[i] += first;
+    for (int j = 0; j < top_k; ++j) {
+        const unsigned top = __reduce_max_sync(kFull, key[0]);
+        if (top == 0) break;
+        const int owner = __ffs(__ballot_sync(kFull, key[0] == top)) - 1;
+        const int e = __shfl_sync(kFull, at[0], owner);
+        if (lane == j) mine = e;
+        if (lane == owner) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = lane * V + i;
-            if (e < p.n_experts && !((kept >> (e / p.group_size)) & 1)) key[i] = 0;
+            for (int i = 0; i + 1 < V; ++i) { key[i] = key[i + 1]; at[i] = at[i + 1]; }
+            key[V - 1] = 0u;
         }
     }
+    __syncwarp();
+    return mine;
 }
 
 // One warp per row, V * 32 experts at most.
-template <typename T, int V>
+template <typename T, int V, int kRouteWarps>
 __device__ __forceinline__ void route_rows(const T *__restrict__ logits, int64_t first, int64_t last, int64_t ld, bool whole,
                                            const float *__restrict__ bias, const RouterParams &p,
                                            int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
                                            int *cta_count, float (*scores)[V * 32], unsigned *__restrict__ status)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ unsigned packed[kRouteWarps][V * 16];
+    __shared__ unsigned char packed_lane[kRouteWarps][32];
     float b[V];
-    bool nan = false, inf = false;
+    unsigned b_off = 0;
+    bool nan = false;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane * V + i;
         b[i] = bias && e < p.n_experts ? clean_logit(bias[e], &nan) : 0.f;
-        inf |= b[i] == -INFINITY;
+        if (b[i] == -INFINITY || e >= p.n_experts) { b_off |= 1u << i; b[i] = 0.f; }
     }
+    // groups of whole lanes; few enough kept that their experts fit half as many places
+    int lanes = 0;
+    if (p.n_groups > 1 && p.group_size % V == 0 && (p.group_size / V & (p.group_size / V - 1)) == 0) lanes = p.group_size / V;
+    const bool halved = V > 1 && lanes && p.top_groups * p.group_size <= 16 * V;
     for (int64_t n = first + warp; n < last; n += blockDim.x >> 5) {
         float s[V];
-        unsigned key[V];
-        load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s, &nan);
-        unsigned off = 0;
+        unsigned key[V], off = 0;
+        if (load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s)) {
+            clean_row<V>(s, &nan);
 #pragma unroll
-        for (int i = 0; i < V; ++i) off |= (s[i] == -INFINITY || (inf && b[i] == -INFINITY) ? 1u : 0u) << i;
+            for (int i = 0; i < V; ++i) off |= (s[i] == -INFINITY ? 1u : 0u) << i;
+        }
         scores_of<V>(s, p.sigmoid);
+        float *row = scores[warp];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            key[i] = (off >> i) & 1 ? 0u : key_of(s[i] + b[i]);
-            scores[warp][lane * V + i] = s[i];
+            key[i] = key_of(s[i] + b[i]);
+            row[lane * V + i] = s[i];
         }
-        if (p.n_groups > 1) keep_groups<V>(key, p, lane);
-        // every round takes the best head of the lanes' sorted lists
-        int my_expert = -1, order[V];                // lane j: slot j
-        sort_lane<V>(key, order);
-        for (int j = 0; j < p.top_k; ++j) {
-            const unsigned top = __reduce_max_sync(kFull, key[0]);
-            if (top == 0) break;
-            const int owner = __ffs(__ballot_sync(kFull, key[0] == top)) - 1;
-            const int e = __shfl_sync(kFull, lane * V + order[0], owner);
-            if (lane == j) my_expert = e;
-            const bool pop = lane == owner;
+        if (off | b_off) {
 #pragma unroll
-            for (int i = 0; i + 1 < V; ++i) { key[i] = pop ? key[i + 1] : key[i]; order[i] = pop ? order[i + 1] : order[i]; }
-            key[V - 1] = pop ? 0u : key[V - 1];
+            for (int i = 0; i < V; ++i) if (((off | b_off) >> i) & 1) key[i] = 0u;
         }
-        __syncwarp();
+        int my_expert;                               // lane j: slot j
+        if (p.n_groups == 1) {
+            my_expert = best_experts<V>(key, lane * V, p.top_k, lane);
+        } else {
+            const unsigned kept = kept_groups<V>(key, p, lanes, lane);
+            if (halved) {
+                // the kept groups' keys move together, V / 2 to a lane
+                constexpr int H = V > 1 ? V / 2 : 1;
+                const int group = lane / lanes, chunk = __popc(kept & ((1u << group) - 1)) * lanes + lane % lanes;
+                if (lane < p.n_groups * lanes && ((kept >> group) & 1)) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) packed[warp][chunk * V + i] = key[i];
+                    packed_lane[warp][chunk] = (unsigned char)lane;
+                }
+                __syncwarp();
+                const bool used = lane / 2 < p.top_groups * lanes;
+                unsigned half[H];
+#pragma unroll
+                for (int i = 0; i < H; ++i) half[i] = used ? packed[warp][lane * H + i] : 0u;
+                const int from = used ? packed_lane[warp][lane / 2] : 0;
+                my_expert = best_experts<H>(half, from * V + lane % 2 * H, p.top_k, lane);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int e = lane * V + i;
+                    if (e < p.n_experts && !((kept >> (e / p.group_size)) & 1)) key[i] = 0u;
+                }
+                my_expert = best_experts<V>(key, lane * V, p.top_k, lane);
+            }
+        }
         const float my_score = my_expert >= 0 ? scores[warp][my_expert] : 0.f;
         const float total = warp_sum(my_score) + kSumFloor;
         if (lane < p.top_k) {
             out_expert[n * p.top_k + lane] = my_expert;
-            out_weight[n * p.top_k + lane] = p.scale * (p.renormalise ? my_score / total : my_score);
+            out_weight[n * p.top_k + lane] = p.scale * (p.renormalise ? __fdividef(my_score, total) : my_score);
             if (cta_count && my_expert >= 0) atomicAdd(&cta_count[my_expert], 1);
         }
         __syncwarp();
@@ -281,7 +339,7 @@ route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bo
     for (int e = threadIdx.x; e < p.n_experts; e += kRouteThreads) cta_count[e] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * rows_per_cta;
-    route_rows<T, V>(logits, first, min(first + rows_per_cta, n_tokens), ld, whole, bias, p, out_expert, out_weight,
+    route_rows<T, V, kRouteThreads / 32>(logits, first, min(first + rows_per_cta, n_tokens), ld, whole, bias, p, out_expert, out_weight,
                      counts ? cta_count : nullptr, scores, status);
     if (!counts) return;
     __syncthreads();
@@ -292,38 +350,41 @@ route_rows_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bo
 
 // Few experts without groups: one thread per row, all of its scores in registers (E of them, the
 // experts or a few more; those past the last are taken out of the choice).
+__host__ __device__ constexpr int fewest_of(int width) { return width <= 4 ? 1 : width <= 12 ? width - 1 : width == 16 ? 13 : width == 24 ? 17 : 25; }
+
 template <typename T, int E>
-__device__ __forceinline__ void load_token(const T *__restrict__ row, int n_experts, float (&x)[E], bool *nan) {
-    bool any = false;
+__device__ __forceinline__ void load_token(const T *__restrict__ row, int n_experts, float (&x)[E]) {
+    constexpr int kAlways = fewest_of(E);            // (a width serves no fewer experts than these)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float v = e < n_experts ? to_float(row[e]) : -INFINITY;
-        any |= v != v;
-        x[e] = fminf(v, kLargest);
-    }
-    if (any) {
-        *nan = true;
-#pragma unroll
-        for (int e = 0; e < E; ++e) if (e < n_experts && to_float(row[e]) != to_float(row[e])) x[e] = -INFINITY;
-    }
+    for (int e = 0; e < E; ++e) x[e] = e < kAlways || e < n_experts ? to_float(row[e]) : -INFINITY;
 }
 
+// Scores up to the factor *inv (softmax: exponentials and one over their sum; sigmoid: 1).
 template <int E>
-__device__ __forceinline__ void token_scores(float (&x)[E], bool sigmoid_score) {
+__device__ __forceinline__ float token_scores_once(const float (&x)[E], float (&s)[E], bool sigmoid_score) {
+    float sum = 0.f;
     if (sigmoid_score) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = sigmoid(x[e]);
-        return;
+        for (int e = 0; e < E; ++e) { s[e] = sigmoid(x[e]); sum += s[e]; }
+        return sum;
     }
-    float top = x[0], sum = 0.f;
+    float top = -kLargest;                           // (a row with nothing left: every exponential is 0)
 #pragma unroll
-    for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
-    top = fmaxf(top, -kLargest);                     // (a row with nothing left: every exponential is 0)
+    for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
 #pragma unroll
-    for (int e = 0; e < E; ++e) { x[e] = expf(x[e] - top); sum += x[e]; }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    for (int e = 0; e < E; ++e) { s[e] = exp2_fast((x[e] - top) * kLog2e); sum += s[e]; }
+    return sum;
+}
+// NaNs and +infinity make the sum a NaN; only then the logits are looked at one by one.
+template <int E>
+__device__ __forceinline__ void token_scores(float (&x)[E], float (&s)[E], bool sigmoid_score, float *inv, bool *nan) {
+    float sum = token_scores_once<E>(x, s, sigmoid_score);
+    if (sum != sum) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] *= inv;
+        for (int e = 0; e < E; ++e) x[e] = clean_logit(x[e], nan);
+        sum = token_scores_once<E>(x, s, sigmoid_score);
+    }
+    *inv = sigmoid_score ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
 }
 
 // count: this thread's column of [experts][threads] counters in shared memory, or null
@@ -332,23 +393,20 @@ __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n
                                             int32_t *__restrict__ out_expert, float *__restrict__ out_weight,
                                             int *count, int stride, bool *nan)
 {
-    float s[E], c[E];                                // score; choice score, -infinity where it cannot be chosen
-    load_token<T, E>(row, p.n_experts, s, nan);
-    unsigned off = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) off |= (s[e] == -INFINITY ? 1u : 0u) << e;
-    token_scores<E>(s, p.sigmoid);
+    // scores up to the factor inv; choice scores, -infinity where an expert cannot be chosen (without a
+    // bias the factor, the same for the whole row, does not change their order)
+    float x[E], s[E], c[E], inv;
+    load_token<T, E>(row, p.n_experts, x);
+    token_scores<E>(x, s, p.sigmoid, &inv, nan);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         c[e] = s[e];
-        if (kBias && e < p.n_experts) c[e] += clean_logit(__ldg(bias + e), nan);
-        if ((off >> e) & 1) c[e] = -INFINITY;
+        if (kBias && e < p.n_experts) c[e] = fmaf(s[e], inv, clean_logit(__ldg(bias + e), nan));
+        if (x[e] == -INFINITY) c[e] = -INFINITY;
     }
     int32_t *experts = out_expert + n * p.top_k;
     float *weights = out_weight + n * p.top_k;
-    float total = kSumFloor;
-    // (weights are written unscaled and read back for the scaling: top_k is small, and so is the cache line)
-    float q0 = 0.f, q1 = 0.f;
+    float total = kSumFloor, q0 = 0.f, q1 = 0.f;     // (two slots' scores stay in registers, more are read back)
     for (int j = 0; j < p.top_k; ++j) {
         float best = -INFINITY, score = 0.f;
         int at = -1;
@@ -356,7 +414,7 @@ __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n
         for (int e = 0; e < E; ++e)
             if (c[e] > best) { best = c[e]; at = e; if (kBias) score = s[e]; }
         if (at >= 0) {
-            if (!kBias) score = best;
+            score = (kBias ? score : best) * inv;
             if (count) count[at * stride] += 1;
 #pragma unroll
             for (int e = 0; e < E; ++e) if (e == at) c[e] = -INFINITY;
@@ -365,10 +423,10 @@ __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n
         total += score;
         if (j == 0) q0 = score; else if (j == 1) q1 = score; else weights[j] = score;
     }
-    const float f = p.scale;
-    weights[0] = f * (p.renormalise ? q0 / total : q0);
-    if (p.top_k > 1) weights[1] = f * (p.renormalise ? q1 / total : q1);
-    for (int j = 2; j < p.top_k; ++j) weights[j] = f * (p.renormalise ? weights[j] / total : weights[j]);
+    const float f = p.renormalise ? __fdividef(p.scale, total) : p.scale;
+    weights[0] = f * q0;
+    if (p.top_k > 1) weights[1] = f * q1;
+    for (int j = 2; j < p.top_k; ++j) weights[j] = f * weights[j];
 }
 
 template <typename T, int E, bool kBias>
@@ -537,7 +595,7 @@ route_small_kernel(const T *__restrict__ logits, int n_tokens, int64_t ld, bool 
             else route_token<T, V, false>(logits + n * ld, n, bias, p, out_expert, out_weight, nullptr, 0, &nan);
         if (nan) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
     } else {
-        route_rows<T, V>(logits, 0, n_tokens, ld, whole, bias, p, out_expert, out_weight, nullptr,
+        route_rows<T, V, kSmallThreads / 32>(logits, 0, n_tokens, ld, whole, bias, p, out_expert, out_weight, nullptr,
                          reinterpret_cast<float (*)[V * 32]>(cnt), status);
     }
     __syncthreads();
@@ -578,7 +636,7 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
     bool bad = false;
     for (int64_t n = (int64_t)blockIdx.x * kWarps + warp; n < n_tokens; n += (int64_t)gridDim.x * kWarps) {
         float s[V];
-        load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s, &bad);
+        if (load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s)) clean_row<V>(s, &bad);
         int e = lane < p.top_k ? expert[n * p.top_k + lane] : -1;
         if (e < -1 || e >= p.n_experts) { bad = true; e = -1; }
         const float dw = e >= 0 ? d_weight[n * p.top_k + lane] : 0.f;
@@ -636,10 +694,12 @@ route_tokens_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int
     dependent_wait();
     bool bad = false;
     for (int64_t n = (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; n < n_tokens; n += (int64_t)gridDim.x * kRouteThreads) {
-        float s[E], ds[E];
-        load_token<T, E>(logits + n * ld, p.n_experts, s, &bad);
-        token_scores<E>(s, p.sigmoid);
+        float x[E], s[E], ds[E], inv;
+        load_token<T, E>(logits + n * ld, p.n_experts, x);
+        token_scores<E>(x, s, p.sigmoid, &inv, &bad);
         unsigned chosen = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] *= inv;
         float sum = kSumFloor, mean = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) ds[e] = 0.f;
@@ -703,7 +763,8 @@ template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a
     const RouterParams p = params_of(a.r);
     const bool tokens = p.n_experts <= kTokenExperts && p.n_groups == 1;
     const T *logits = (const T *)a.logits;
-    if (a.offsets && a.n_tokens <= (tokens ? 2 * kSmallThreads : kSmallThreads / 32 * 8)) {
+    // one CTA: two tokens a thread, or eight rows a warp (its tables fit 48 KB up to 256 experts)
+    if (a.offsets && a.n_tokens <= (tokens ? 2 * kSmallThreads : p.n_experts <= 256 ? kSmallThreads / 32 * 8 : -1)) {
         const size_t counters = sizeof(int) * (kSmallThreads / 32) * (size_t)p.n_experts, lead = sizeof(int) * (p.n_experts + 1);
         LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
         if (tokens)
@@ -713,7 +774,7 @@ template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a
                                         a.token_row, ctx->s.status);
             });
         return by_row_width(p.n_experts, [&](auto v) {
-            constexpr int V = decltype(v)::value;
+            constexpr int V = decltype(v)::value < 16 ? decltype(v)::value : 8;
             const size_t scores = sizeof(float) * (kSmallThreads / 32) * V * 32;
             return launch_dependent(route_small_kernel<T, V, false>, dim3(1), dim3(kSmallThreads), lead + (counters > scores ? counters : scores), st,
                                     logits, (int)a.n_tokens, a.ld, whole_rows<T, V>(a.ld, p.n_experts), a.bias, p, a.expert, a.weight,
@@ -721,7 +782,7 @@ template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a
         });
     }
     const int at_once = tokens ? kRouteThreads : kRouteThreads / 32;         // rows of a CTA
-    const int64_t want = (a.n_tokens + at_once - 1) / at_once;
+    const int64_t want = a.n_tokens < 1 ? 1 : (a.n_tokens + at_once - 1) / at_once;
     const int n_ctas = want < route_ctas(ctx) ? (int)want : route_ctas(ctx);
     const int rows_per_cta = (int)(((a.n_tokens + n_ctas - 1) / n_ctas + at_once - 1) / at_once * at_once);
     int *counts = a.offsets ? operator_scratch(ctx).expert_counts : nullptr;
