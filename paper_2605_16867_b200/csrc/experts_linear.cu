@@ -307,8 +307,8 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     __syncthreads();
     if (*failed) {
         if (threadIdx.x == 0) atomicOr(p.status, (unsigned)GS_DEV_TIMEOUT);
-        const uint64_t start = now_ns();
-        while (now_ns() - start < 1000000ull) { }
+        const long long start = clock64();
+        while (clock64() - start < 2000000ll) { }
     }
     __syncwarp();
     cluster_sync();
@@ -328,9 +328,9 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 // instructions may read them.  db is one more product, with a block of ones, for the tiles of the
 // first in features.
 
-constexpr int kMinPiece = 32;                   // steps of 64 rows; an expert is not cut finer
-constexpr int kPiecesPerPair = 1;
-constexpr int kChain = 8;                       // steps
+constexpr int kMinPiece = 48;                   // steps of 64 rows; an expert is not cut finer
+constexpr int kPiecesPerPair = 3;
+constexpr int kChain = 12;                       // steps
 // Warps: 0 copies, 1 issues the matrix instructions, 2 clears; the last eight store.  With gathered
 // rows 3 to 7 issue the gathers, and registers move from the first eight warps to the storing ones
 // (which hold 128 sums a thread): 256 * 56 + 256 * 184 of the 512 * 128 that the block starts with.
@@ -685,8 +685,8 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
     __syncthreads();
     if (*failed) {
         if (threadIdx.x == 0) atomicOr(p.status, (unsigned)GS_DEV_TIMEOUT);
-        const uint64_t start = now_ns();
-        while (now_ns() - start < 1000000ull) { }
+        const long long start = clock64();
+        while (clock64() - start < 2000000ll) { }
     }
     __syncwarp();
     cluster_sync();

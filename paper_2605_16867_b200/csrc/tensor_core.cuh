@@ -13,7 +13,7 @@ namespace gs {
 namespace tc {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr uint64_t kWaitLimitNs = 4000000000ull;     // a wait that takes this long has failed
+constexpr long long kWaitLimit = 8000000000ll;       // cycles (four seconds or more): a wait that takes this long has failed
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -54,22 +54,17 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ uint64_t now_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
 // Waits for the phase of the given parity.  False: this wait, or another of the CTA, took too long
 // (*failed is set): the caller leaves its loop and the kernel ends.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
-    if (bar_try(bar, parity)) return true;
-    const uint64_t start = now_ns();
-    for (;;) {
+#pragma unroll 1
+    for (long long start = 0;;) {
 #pragma unroll 1
         for (int i = 0; i < 64; ++i)
             if (bar_try(bar, parity)) return true;
         if (*failed) return false;
-        if (now_ns() - start > kWaitLimitNs) { *failed = 1; return false; }
+        if (start == 0) start = clock64();
+        else if (clock64() - start > kWaitLimit) { *failed = 1; return false; }
     }
 }
 
