@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -51,10 +52,6 @@ class _InstanceTable(C.Structure):
 class _ExpertRouter(C.Structure):
     _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("n_groups", C.c_int32),
                 ("top_groups", C.c_int32), ("group_top", C.c_int32), ("renormalise", C.c_int32), ("scale", C.c_float)]
-
-
-class _Grad(C.Structure):
-    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n_elements", C.c_int64), ("dtype", C.c_int32)]
 
 
 class _InstancesMut(C.Structure):
@@ -184,48 +181,57 @@ def _host_ptr(a, dtype, n: Optional[int], name: str) -> Optional[int]:
     return a.ctypes.data
 
 
+# the current stream's cudaStream_t (torch.cuda.current_stream builds an object around it)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _OPERANDS = (torch.bfloat16, torch.float16)
 
 
-def _array(t, dtype: torch.dtype, n: int, name: str, device) -> Optional[int]:
-    """A contiguous CUDA tensor of n elements, whatever its shape."""
+def _refuse(t, dtype, shape, name: str, index: int):
+    """Says what is wrong with an argument that one of the checks below turned down."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != index:
+        raise TypeError(f"{name}: expected a tensor on cuda:{index}")
+    if t.dtype is not dtype or (isinstance(shape, tuple) and t.dim() != len(shape)):
+        raise TypeError(f"{name}: expected a {len(shape)}-D {dtype} tensor, got {t.dtype} {tuple(t.shape)}"
+                        if isinstance(shape, tuple) else f"{name}: expected a {dtype} tensor, got {t.dtype}")
+    if isinstance(shape, tuple) and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected {list(shape)}, got {list(t.shape)}")
+    if not isinstance(shape, tuple) and t.numel() != shape:
+        raise ValueError(f"{name}: needs {shape} elements, has {t.numel()}")
+    raise TypeError(f"{name}: expected evenly spaced rows of consecutive elements, got strides {t.stride()}")
+
+
+# (These run before every launch of a few microseconds: one expression on the way that is taken, and
+# all explanations on the other one.)
+def _array(t, dtype: torch.dtype, n: int, name: str, index: int) -> Optional[int]:
+    """The address of a contiguous CUDA tensor of n elements, whatever its shape."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise TypeError(f"{name}: expected a tensor on {device}")
-    if t.dtype is not dtype or not t.is_contiguous():
-        raise TypeError(f"{name}: expected a contiguous {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
-    if t.numel() != n:
-        raise ValueError(f"{name}: needs {n} elements, has {t.numel()}")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.is_cuda
+            and t.get_device() == index):
+        _refuse(t, dtype, n, name, index)
     return t.data_ptr()
 
 
-def _matrix(t, dtype: torch.dtype, rows: int, cols: int, name: str, device):
+def _matrix(t, dtype: torch.dtype, rows: int, cols: int, name: str, index: int):
     """(address, row stride) of a row-major CUDA matrix; the rows may be further apart than they are wide."""
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise TypeError(f"{name}: expected a tensor on {device}")
-    if t.dtype is not dtype or t.dim() != 2:
-        raise TypeError(f"{name}: expected a 2-D {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name}: expected [{rows}, {cols}], got {tuple(t.shape)}")
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == (rows, cols) and t.is_cuda and t.get_device() == index):
+        _refuse(t, dtype, (rows, cols), name, index)
     ld, one = t.stride()
     if (one != 1 and cols > 1) or (ld < cols and rows > 1):
-        raise TypeError(f"{name}: expected rows of consecutive elements, got strides {t.stride()}")
-    return t.data_ptr(), ld if rows > 1 or ld >= cols else (cols + 7) // 8 * 8
+        _refuse(t, dtype, (rows, cols), name, index)
+    return t.data_ptr(), ld if ld >= cols else (cols + 7) // 8 * 8
 
 
-def _stack(t, dtype: torch.dtype, name: str, device):
-    """(address, row stride) of the experts' matrices [experts, out, in], out rows apart."""
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise TypeError(f"{name}: expected a tensor on {device}")
-    if t.dtype is not dtype or t.dim() != 3:
-        raise TypeError(f"{name}: expected a 3-D {dtype} tensor, got {t.dtype} {tuple(t.shape)}")
-    (e, o, i), (step, ld, one) = t.shape, t.stride()
+def _stack(t, dtype: torch.dtype, shape, name: str, index: int):
+    """(address, row stride) of the experts' matrices [experts, out, in], experts out rows apart."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and len(shape) == 3 and t.is_cuda and t.get_device() == index):
+        _refuse(t, dtype, tuple(shape) if len(shape) == 3 else (0, 0, 0), name, index)
+    (e, o, i), (step, ld, one) = shape, t.stride()
     if o == 1:
         ld = step if e > 1 else max(ld, (i + 7) // 8 * 8)
     if (one != 1 and i > 1) or ld < i or (e > 1 and step != o * ld):
-        raise TypeError(f"{name}: expected evenly spaced rows of consecutive elements, got strides {t.stride()}")
+        _refuse(t, dtype, tuple(shape), name, index)
     return t.data_ptr(), ld
 
 
@@ -279,7 +285,7 @@ class GoodServe:
         if not torch.cuda.is_available():
             raise RuntimeError("GoodServe needs a CUDA device; there is no CPU implementation")
         self._lib = load_library(counting=counting, checking=checking)
-        self.device = torch.device("cuda", device)
+        self.device, self._index = torch.device("cuda", device), int(device)
         torch.cuda.init()
         with torch.cuda.device(self.device):
             torch.zeros(1, device=self.device)          # make sure the primary context exists
@@ -290,7 +296,7 @@ class GoodServe:
 
     # -- plumbing ------------------------------------------------------------------------
     def _check(self, rc: int):
-        if rc != 0:
+        if rc:
             raise GoodServeError(rc, self._lib.gs_strerror(rc).decode())
 
     def _stream(self, stream) -> Optional[int]:
@@ -522,7 +528,7 @@ class GoodServe:
         """gs_expert_route.  logits [tokens, experts] (float32, bfloat16 or float16; any row stride);
         out_expert, out_weight and out_token_row [tokens, top_k], out_offsets [experts + 1],
         out_row_token [tokens * top_k]; the last three together or not at all."""
-        dev, i32 = self.device, torch.int32
+        dev, i32 = self._index, torch.int32
         code = _DTYPES.get(logits.dtype)
         if code is None:
             raise TypeError(f"logits: expected float32, bfloat16 or float16, got {logits.dtype}")
@@ -532,11 +538,11 @@ class GoodServe:
             self._h, x, code, n, ld, _array(bias, torch.float32, e, "bias", dev), router._address,
             _array(out_expert, i32, n * k, "out_expert", dev), _array(out_weight, torch.float32, n * k, "out_weight", dev),
             _array(out_offsets, i32, e + 1, "out_offsets", dev), _array(out_row_token, i32, n * k, "out_row_token", dev),
-            _array(out_token_row, i32, n * k, "out_token_row", dev), self._stream(stream)))
+            _array(out_token_row, i32, n * k, "out_token_row", dev), _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def expert_route_backward(self, logits, router: ExpertRouter, expert, d_weight, out_d_logits, stream=None):
         """gs_expert_route_backward: d_weight [tokens, top_k] to out_d_logits [tokens, experts]."""
-        dev, n, e, k = self.device, logits.shape[0], router.n_experts, router.top_k
+        dev, n, e, k = self._index, logits.shape[0], router.n_experts, router.top_k
         code = _DTYPES.get(logits.dtype)
         if code is None:
             raise TypeError(f"logits: expected float32, bfloat16 or float16, got {logits.dtype}")
@@ -544,15 +550,15 @@ class GoodServe:
         d, ld_d = _matrix(out_d_logits, logits.dtype, n, e, "out_d_logits", dev)
         self._check(self._lib.gs_expert_route_backward(
             self._h, x, code, n, ld, router._address, _array(expert, torch.int32, n * k, "expert", dev),
-            _array(d_weight, torch.float32, n * k, "d_weight", dev), d, ld_d, self._stream(stream)))
+            _array(d_weight, torch.float32, n * k, "d_weight", dev), d, ld_d, _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def expert_linear(self, x, w, offsets, out, bias=None, row_token=None, relu: bool = False, stream=None):
         """gs_expert_linear: out[r] = act(x[row_token[r]] . w[e]^T + bias[e]) for the rows r of expert e.
         w [experts, out, in]; without row_token x has a row for every row of out."""
-        dev, dt = self.device, x.dtype
+        dev, dt = self._index, x.dtype
         if dt not in _OPERANDS:
             raise TypeError(f"x: expected bfloat16 or float16, got {dt}")
-        wp, ldw = _stack(w, dt, "w", dev)
+        wp, ldw = _stack(w, dt, w.shape, "w", dev)
         e, o, i = w.shape
         rows, nx = out.shape[0], x.shape[0]
         xp, ldx = _matrix(x, dt, nx, i, "x", dev)
@@ -560,17 +566,17 @@ class GoodServe:
         self._check(self._lib.gs_expert_linear(
             self._h, _DTYPES[dt], xp, nx, ldx, _array(row_token, torch.int32, rows, "row_token", dev),
             _array(offsets, torch.int32, e + 1, "offsets", dev), e, rows, wp, ldw,
-            _array(bias, torch.float32, e * o, "bias", dev), i, o, 1 if relu else 0, yp, ldy, self._stream(stream)))
+            _array(bias, torch.float32, e * o, "bias", dev), i, o, 1 if relu else 0, yp, ldy, _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def expert_linear_backward(self, dz, x, w, offsets, dx=None, dw=None, db=None, row_token=None,
                                relu_input: bool = False, stream=None):
         """gs_expert_linear_backward: fills those of dx [rows, in], dw [experts, out, in] (float32) and
         db [experts, out] (float32) that are given.  The partial sums' workspace comes from PyTorch's
         allocator, on the stream of the call."""
-        dev, dt = self.device, dz.dtype
+        dev, dt = self._index, dz.dtype
         if dt not in _OPERANDS:
             raise TypeError(f"dz: expected bfloat16 or float16, got {dt}")
-        wp, ldw = _stack(w, dt, "w", dev)
+        wp, ldw = _stack(w, dt, w.shape, "w", dev)
         e, o, i = w.shape
         rows, nx = dz.shape[0], x.shape[0]
         zp, ldz = _matrix(dz, dt, rows, o, "dz", dev)
@@ -580,23 +586,21 @@ class GoodServe:
         if dx is not None:
             dxp, lddx = _matrix(dx, dt, rows, i, "dx", dev)
         if dw is not None:
-            if dw.shape != w.shape:
-                raise ValueError(f"dw: expected {tuple(w.shape)}, got {tuple(dw.shape)}")
-            dwp, lddw = _stack(dw, torch.float32, "dw", dev)
+            dwp, lddw = _stack(dw, torch.float32, w.shape, "dw", dev)
             need = self._lib.gs_expert_linear_backward_workspace(self._h, e, rows, i, o)
             if need > 0:
-                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
                 if stream is not None:
                     workspace.record_stream(stream)
         self._check(self._lib.gs_expert_linear_backward(
             self._h, _DTYPES[dt], zp, ldz, xp, nx, ldx, _array(row_token, torch.int32, rows, "row_token", dev),
             _array(offsets, torch.int32, e + 1, "offsets", dev), e, rows, wp, ldw, i, o, 2 if relu_input else 0,
             dxp, lddx, dwp, lddw, _array(db, torch.float32, e * o, "db", dev),
-            None if workspace is None else workspace.data_ptr(), max(need, 0), self._stream(stream)))
+            None if workspace is None else workspace.data_ptr(), max(need, 0), _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def expert_combine(self, y, token_row, out, weight=None, stream=None):
         """gs_expert_combine: out[n] = sum over j of weight[n, j] * y[token_row[n, j]]; out in y's dtype or float32."""
-        dev, dt = self.device, y.dtype
+        dev, dt = self._index, y.dtype
         if dt not in _OPERANDS:
             raise TypeError(f"y: expected bfloat16 or float16, got {dt}")
         if out.dtype is not dt and out.dtype is not torch.float32:
@@ -606,12 +610,12 @@ class GoodServe:
         op, ldo = _matrix(out, out.dtype, n, f, "out", dev)
         self._check(self._lib.gs_expert_combine(
             self._h, _DTYPES[dt], yp, rows, ldy, _array(token_row, torch.int32, n * k, "token_row", dev),
-            _array(weight, torch.float32, n * k, "weight", dev), n, k, f, _DTYPES[out.dtype], op, ldo, self._stream(stream)))
+            _array(weight, torch.float32, n * k, "weight", dev), n, k, f, _DTYPES[out.dtype], op, ldo, _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def expert_combine_backward(self, d_out, y, token_row, dy=None, weight=None, d_weight=None, relu: bool = False,
                                 stream=None):
         """gs_expert_combine_backward: fills those of dy [rows, features] and d_weight [tokens, top_k] that are given."""
-        dev, dt = self.device, y.dtype
+        dev, dt = self._index, y.dtype
         if dt not in _OPERANDS:
             raise TypeError(f"y: expected bfloat16 or float16, got {dt}")
         if d_out.dtype is not dt and d_out.dtype is not torch.float32:
@@ -623,7 +627,7 @@ class GoodServe:
         self._check(self._lib.gs_expert_combine_backward(
             self._h, _DTYPES[dt], _DTYPES[d_out.dtype], gp, ldg, yp, rows, ldy,
             _array(token_row, torch.int32, n * k, "token_row", dev), _array(weight, torch.float32, n * k, "weight", dev),
-            n, k, f, 2 if relu else 0, dyp, lddy, _array(d_weight, torch.float32, n * k, "d_weight", dev), self._stream(stream)))
+            n, k, f, 2 if relu else 0, dyp, lddy, _array(d_weight, torch.float32, n * k, "d_weight", dev), _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def clip_grad_norm(self, grads, max_norm: float, out_norm, outs=None, write: bool = True, stream=None):
         """gs_clip_grad_norm over contiguous tensors (float32, bfloat16 or float16): scales them in place, or into
@@ -631,19 +635,24 @@ class GoodServe:
         ``write=False`` only the norm is computed."""
         if outs is not None and len(outs) != len(grads):
             raise ValueError(f"outs: needs {len(grads)} tensors, has {len(outs)}")
-        table, dev = (_Grad * len(grads))(), self.device
+        flat, dev = [], self._index                    # four words for every gs_grad
         for k, g in enumerate(grads):
-            code = _DTYPES.get(g.dtype)
-            if code is None or g.device != dev or not g.is_contiguous():
-                raise TypeError(f"grads[{k}]: expected a contiguous float32, bfloat16 or float16 tensor on {dev}")
-            o = g
+            code, n, p = _DTYPES.get(g.dtype), g.numel(), g.data_ptr()
+            if code is None or not g.is_cuda or g.get_device() != dev or not g.is_contiguous():
+                raise TypeError(f"grads[{k}]: expected a contiguous float32, bfloat16 or float16 tensor on cuda:{dev}")
             if outs is not None:
                 o = outs[k]
-                if o.dtype is not g.dtype or o.device != dev or not o.is_contiguous() or o.numel() != g.numel():
-                    raise TypeError(f"outs[{k}]: expected a contiguous {g.dtype} tensor of {g.numel()} elements on {dev}")
-            table[k] = (g.data_ptr(), o.data_ptr() if write else None, g.numel(), code)
-        self._check(self._lib.gs_clip_grad_norm(self._h, C.addressof(table), len(grads), float(max_norm),
-                                                _array(out_norm, torch.float32, 1, "out_norm", dev), self._stream(stream)))
+                if o.dtype is not g.dtype or o.numel() != n or not o.is_cuda or o.get_device() != dev or not o.is_contiguous():
+                    raise TypeError(f"outs[{k}]: expected a contiguous {g.dtype} tensor of {n} elements on cuda:{dev}")
+                flat += (p, o.data_ptr(), n, code)
+            else:
+                flat += (p, p if write else 0, n, code)
+        if outs is not None and not write:
+            flat[1::4] = [0] * len(grads)
+        table = array("q", flat)
+        self._check(self._lib.gs_clip_grad_norm(self._h, table.buffer_info()[0], len(grads), float(max_norm),
+                                                _array(out_norm, torch.float32, 1, "out_norm", dev),
+                                                _raw_stream(dev) if stream is None else stream.cuda_stream))
 
     def device_status(self, stream=None) -> int:
         bits = C.c_uint(0)

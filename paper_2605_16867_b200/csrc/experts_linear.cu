@@ -228,14 +228,23 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
         // lanes of tensor memory that this warp reads, and its columns
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         constexpr int kCols = kN / (S::kStoreWarps / 4);
-        T *mine = reinterpret_cast<T *>(store + (warp - 2) * 2048);
+        // a block of 32 requests x 32 features passes through shared memory: request i's four pieces of
+        // eight features lie in turned order, so that neither side meets a bank twice
+        unsigned char *mine = store + (warp - 2) * 2048;
+        const uint32_t put = smem_u32(mine) + lane % 8 * 64 + ((lane / 8 ^ (lane % 8 >> 1)) & 3) * 16;
+        const unsigned char *get = mine + lane / 4 * 64 + ((lane ^ (lane / 4 >> 1)) & 3) * 16;
         int e = 0, use = 0;
         bool bad = false;
         for (int64_t t = pair; t < n_tiles; t += n_pairs, ++use) {
             const int rt = (int)(t / m_tiles), f0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM + quarter * 32;
             while (tile_start[e + 1] <= rt) ++e;
             const int r0 = row_start[e] + (rt - tile_start[e]) * kN + half * kCols, r1 = min(r0 + kCols, row_end[e]);
-            const float add = p.bias && f0 + lane < p.features ? p.bias[(int64_t)e * p.features + f0 + lane] : 0.f;
+            float add[4];                                     // of features l / 4 + 8 i, as the sums come
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int f = f0 + i * 8 + lane / 4;
+                add[i] = !kDx && p.bias && f < p.features ? p.bias[(int64_t)e * p.features + f] : 0.f;
+            }
             // a lane's four pieces of a block of 32 requests: eight features of request i * 8 + lane / 4 each
             const int f = f0 + lane % 4 * 8, width = min(8, p.features - f);
             uint4 keep[4];                                    // the mask's values there, asked for a block ahead
@@ -257,19 +266,23 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 #pragma unroll 1
             for (int c = 0; c < kCols; c += 32) {
                 if (r0 + c >= r1 || f0 >= p.features) break;
-                float v[32];
-                tmem_load32(sums + c, v);
+                uint32_t lo[16], hi[16];                      // features 0-15 and 16-31 of the warp's 32
+                tmem_load_fragments(sums + c, lo);
+                tmem_load_fragments(sums + c + (16u << 16), hi);
+                tmem_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float z = v[i] + add;
-                    if (!kDx && p.relu) z = z > 0.f || z != z ? z : 0.f;
-                    mine[i * 32 + lane] = from_float<T>(z);
+                for (int j = 0; j < 4; ++j) {                 // eight requests
+                    const auto out = [&](const uint32_t *r, float b) {
+                        const uint32_t z = pack2<T>(__uint_as_float(r[0]) + b, __uint_as_float(r[1]) + b);
+                        return !kDx && p.relu ? relu2<T>(z) : z;
+                    };
+                    store_transposed(put + j * 512, out(lo + 4 * j, add[0]), out(lo + 4 * j + 2, add[1]), out(hi + 4 * j, add[2]), out(hi + 4 * j + 2, add[3]));
                 }
                 __syncwarp();
                 uint4 q[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    q[i] = *reinterpret_cast<const uint4 *>(mine + (i * 32 + lane) * 8);
+                    q[i] = *reinterpret_cast<const uint4 *>(get + i * 512);
                     if (kDx && p.mask) {
                         T *z = reinterpret_cast<T *>(&q[i]);
                         const T *x = reinterpret_cast<const T *>(&keep[i]);

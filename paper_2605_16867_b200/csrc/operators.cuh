@@ -32,6 +32,30 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// Two floats rounded to T, the first in the low half.
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// max(v, 0) of both halves; a NaN stays one.
+template <typename T> __device__ __forceinline__ uint32_t relu2(uint32_t v);
+template <> __device__ __forceinline__ uint32_t relu2<__nv_bfloat16>(uint32_t v) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0u));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t relu2<__half>(uint32_t v) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0u));
+    return r;
+}
+
 // First and last of a kernel launched with launch_dependent: the kernel after this one may be set
 // up, and this one waits until everything before it in the stream is done and visible.
 __device__ __forceinline__ void dependent_begin() {
