@@ -10,19 +10,21 @@ namespace gs {
 namespace {
 
 constexpr int kClipThreads = 512;
-constexpr int kClipTensors = 256;                    // tensors of one launch (their table travels as a kernel argument)
+constexpr int kClipTensors = 256;                    // tensors of one launch at most (their table travels as a kernel argument,
+constexpr int kClipFew = 32;                         //  and a short one travels faster)
 constexpr int kClipChunk = 16384;                    // elements that a CTA takes at a time
 
-struct ClipTable {
+template <int kMost> struct ClipTable {
     int n;
-    int chunk_start[kClipTensors + 1];               // chunks before each tensor
-    const void *grad[kClipTensors];
-    void *out[kClipTensors];
-    int64_t n_elements[kClipTensors];
-    unsigned char dtype[kClipTensors];
+    int chunk_start[kMost + 1];                      // chunks before each tensor
+    const void *grad[kMost];
+    void *out[kMost];
+    int64_t n_elements[kMost];
+    unsigned char dtype[kMost];
 };
 
-__device__ __forceinline__ int tensor_of(const ClipTable &t, int chunk) {
+template <int kMost>
+__device__ __forceinline__ int tensor_of(const ClipTable<kMost> &t, int chunk) {
     int lo = 0, hi = t.n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -116,8 +118,9 @@ __device__ __forceinline__ double block_sum(double v) {
     return sum;
 }
 
+template <int kMost>
 __global__ void __launch_bounds__(kClipThreads)
-norm_kernel(const __grid_constant__ ClipTable t, double *__restrict__ partials)
+norm_kernel(const __grid_constant__ ClipTable<kMost> t, double *__restrict__ partials)
 {
     dependent_begin();
     double sum = 0.0;
@@ -147,8 +150,9 @@ __device__ __forceinline__ float clip_factor(const double *__restrict__ partials
     return finite ? fminf(1.f, max_norm / (norm + 1e-6f)) : 1.f;
 }
 
+template <int kMost>
 __global__ void __launch_bounds__(kClipThreads)
-clip_kernel(const __grid_constant__ ClipTable t, const double *__restrict__ partials, int n_partials, float max_norm,
+clip_kernel(const __grid_constant__ ClipTable<kMost> t, const double *__restrict__ partials, int n_partials, float max_norm,
             float *__restrict__ out_norm, unsigned *__restrict__ status)
 {
     dependent_begin();
@@ -165,27 +169,25 @@ clip_kernel(const __grid_constant__ ClipTable t, const double *__restrict__ part
     }
 }
 
-}  // namespace
-
-cudaError_t launch_clip(gs_ctx *ctx, const gs_grad *grads, int n_tensors, float max_norm, bool write,
-                        float *out_norm, cudaStream_t st)
+template <int kMost>
+cudaError_t launch_tables(gs_ctx *ctx, const gs_grad *grads, int n_tensors, float max_norm, bool write, float *out_norm, cudaStream_t st)
 {
     // pass 0: partial sums of every table; pass 1: the factor and the values
     double *partials = operator_scratch(ctx).clip_partials;
-    int n_tables = (n_tensors + kClipTensors - 1) / kClipTensors;
-    if (n_tables < 1) n_tables = 1;
+    const int n_tables = n_tensors > kMost ? (n_tensors + kMost - 1) / kMost : 1;
     int per_table = kMaxClipCtas / n_tables;
     if (per_table > ctx->n_sm * 4) per_table = ctx->n_sm * 4;
     if (per_table < 1) return cudaErrorInvalidValue;
     int n_partials = 0;
     for (int pass = 0; pass < 2; ++pass) {
-        for (int first = 0, table = 0; table < n_tables; first += kClipTensors, ++table) {
+        for (int table = 0; table < n_tables; ++table) {
             if (pass == 1 && !write && table > 0) break;
-            ClipTable t;
+            ClipTable<kMost> t;
             t.n = 0;
             t.chunk_start[0] = 0;
             int64_t chunks = 0;
-            for (int i = first; i < n_tensors && i < first + kClipTensors; ++i) {
+            const int last = n_tensors < (table + 1) * kMost ? n_tensors : (table + 1) * kMost;
+            for (int i = table * kMost; i < last && (pass == 0 || write); ++i) {
                 if (grads[i].n_elements == 0) continue;
                 t.grad[t.n] = grads[i].grad;
                 t.out[t.n] = grads[i].out;
@@ -195,21 +197,29 @@ cudaError_t launch_clip(gs_ctx *ctx, const gs_grad *grads, int n_tensors, float 
                 if (chunks > INT32_MAX) return cudaErrorInvalidValue;
                 t.chunk_start[++t.n] = (int)chunks;
             }
-            if (pass == 1 && !write) { t.n = 0; chunks = 0; }
             const int ctas = chunks < 1 ? 1 : chunks < per_table ? (int)chunks : per_table;
             LaunchTimer timer(ctx, GS_K_CLIP, st);
             cudaError_t e;
             if (pass == 0) {
-                e = launch_dependent(norm_kernel, dim3(ctas), dim3(kClipThreads), 0, st, t, partials + n_partials);
+                e = launch_dependent(norm_kernel<kMost>, dim3(ctas), dim3(kClipThreads), 0, st, t, partials + n_partials);
                 n_partials += ctas;
             } else {
-                e = launch_dependent(clip_kernel, dim3(ctas), dim3(kClipThreads), 0, st, t, (const double *)partials,
+                e = launch_dependent(clip_kernel<kMost>, dim3(ctas), dim3(kClipThreads), 0, st, t, (const double *)partials,
                                      n_partials, max_norm, table == 0 ? out_norm : nullptr, ctx->s.status);
             }
             if (e != cudaSuccess) return e;
         }
     }
     return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_clip(gs_ctx *ctx, const gs_grad *grads, int n_tensors, float max_norm, bool write,
+                        float *out_norm, cudaStream_t st)
+{
+    return n_tensors <= kClipFew ? launch_tables<kClipFew>(ctx, grads, n_tensors, max_norm, write, out_norm, st)
+                                 : launch_tables<kClipTensors>(ctx, grads, n_tensors, max_norm, write, out_norm, st);
 }
 
 }  // namespace gs

@@ -263,12 +263,14 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             if (!warp_wait(smem_u32(&bars->sums_full[use & 1]), (use >> 1) & 1, failed)) break;
             fence_after();
             const uint32_t sums = tmem + (use & 1) * kN + half * kCols + ((uint32_t)(quarter * 32) << 16);
+            const int end = f0 < p.features ? min(kCols, r1 - r0) : 0;
+            uint32_t lo[16], hi[16];                          // features 0-15 and 16-31 of the warp's 32
+            if (end > 0) {
+                tmem_load_fragments(sums, lo);
+                tmem_load_fragments(sums + (16u << 16), hi);
+            }
 #pragma unroll 1
-            for (int c = 0; c < kCols; c += 32) {
-                if (r0 + c >= r1 || f0 >= p.features) break;
-                uint32_t lo[16], hi[16];                      // features 0-15 and 16-31 of the warp's 32
-                tmem_load_fragments(sums + c, lo);
-                tmem_load_fragments(sums + c + (16u << 16), hi);
+            for (int c = 0; c < end; c += 32) {
                 tmem_wait();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {                 // eight requests
@@ -277,6 +279,14 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                         return !kDx && p.relu ? relu2<T>(z) : z;
                     };
                     store_transposed(put + j * 512, out(lo + 4 * j, add[0]), out(lo + 4 * j + 2, add[1]), out(hi + 4 * j, add[2]), out(hi + 4 * j + 2, add[3]));
+                }
+                if (c + 32 < end) {                           // the next block's sums come while this one's leave
+                    tmem_load_fragments(sums + c + 32, lo);
+                    tmem_load_fragments(sums + c + 32 + (16u << 16), hi);
+                } else {
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
                 }
                 __syncwarp();
                 uint4 q[4];
@@ -290,7 +300,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                         for (int j = 0; j < 8; ++j) if (width == 8 && !(to_float(x[j]) > 0.f)) z[j] = from_float<T>(0.f);
                     }
                 }
-                if (kDx && p.mask) ask(c + 32);
+                if (kDx && p.mask && c + 32 < end) ask(c + 32);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = r0 + c + i * 8 + lane / 4;
@@ -307,9 +317,11 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                 }
                 __syncwarp();
             }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
+            if (end <= 0) {                                   // nothing of this tile is the warp's
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
+            }
         }
         if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     }
