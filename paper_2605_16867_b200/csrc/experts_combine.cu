@@ -13,8 +13,6 @@ namespace {
 constexpr int kCombineThreads = 256;
 constexpr unsigned kFull = 0xFFFFFFFFu;
 
-template <typename T> struct Eight { T v[8]; };
-
 // Eight columns from `col`; the row is 16-byte aligned and holds `features` of them.
 template <typename T>
 __device__ __forceinline__ void load8(const T *__restrict__ row, int col, int features, float (&v)[8]) {
@@ -53,37 +51,115 @@ __device__ __forceinline__ void store8(T *__restrict__ row, int col, int feature
     }
 }
 
-// kLanes lanes own a token (the fewest that cover its columns, a warp at most).
+// Eight columns as they lie in memory (16-bit values), zeros past the last one.
+template <typename T>
+__device__ __forceinline__ uint4 load_packed(const T *__restrict__ row, int col, int features) {
+    if (col + 8 <= features) return __ldg(reinterpret_cast<const uint4 *>(row + col));
+    uint4 q = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (col + i < features) reinterpret_cast<T *>(&q)[i] = row[col + i];
+    return q;
+}
+
+// Rows and weights of a token's slots: lane j of the token's lanes holds slot j (or, where a token has
+// fewer lanes than slots, they are read where they are used).  The next token's are asked for while
+// this one's rows are on their way: otherwise every token waits for memory twice.
+template <int kLanes>
+struct Slots {
+    static constexpr bool kHeld = kLanes >= GS_MAX_TOP_K;
+    const int32_t *__restrict__ token_row;
+    const float *__restrict__ weight;
+    int64_t n_tokens;
+    int top_k, n_rows, r = -1;
+    float w = 0.f;
+    bool bad = false;
+    __device__ __forceinline__ int checked(int row) {
+        if (row < -1 || row >= n_rows) { bad = true; return -1; }
+        return row;
+    }
+    __device__ __forceinline__ void ask(int64_t n, int part) {
+        if (!kHeld) return;
+        const bool there = n < n_tokens && part < top_k;
+        r = there ? token_row[n * top_k + part] : -1;
+        w = there ? weight ? weight[n * top_k + part] : 1.f : 0.f;
+    }
+    // slot j of token n, from the values asked for (held) or from memory; -1: none
+    __device__ __forceinline__ int row(int64_t n, int j, int held) {
+        if (kHeld) { const int v = __shfl_sync(kFull, held, j & (kLanes - 1), kLanes); return j < top_k ? v : -1; }
+        return n < n_tokens && j < top_k ? checked(token_row[n * top_k + j]) : -1;
+    }
+    __device__ __forceinline__ float factor(int64_t n, int j, float held) {
+        if (kHeld) return __shfl_sync(kFull, held, j & (kLanes - 1), kLanes);
+        return n < n_tokens && j < top_k ? weight ? weight[n * top_k + j] : 1.f : 0.f;
+    }
+};
+
+// kLanes lanes own a token (the fewest that cover its columns, a warp at most).  A lane has kBlocks
+// blocks of eight columns of kSlots slots under way at a time; more in flight costs more warps than it
+// brings (four blocks as floats, 112 registers: 328 us instead of 162 us at 131,072 x 1024).
+constexpr int kBlocks = 2, kSlots = 2;
 template <typename T, typename O, int kLanes>
-__global__ void __launch_bounds__(kCombineThreads)
+__global__ void __launch_bounds__(kCombineThreads, 4)
 combine_kernel(const T *__restrict__ y, int n_rows, int64_t ld_y, const int32_t *__restrict__ token_row,
                const float *__restrict__ weight, int64_t n_tokens, int top_k, int features,
                O *__restrict__ out, int64_t ld_out, unsigned *__restrict__ status)
 {
     dependent_begin();
     const int part = threadIdx.x % kLanes;
-    bool bad = false;
-    for (int64_t n = ((int64_t)blockIdx.x * kCombineThreads + threadIdx.x) / kLanes; n < n_tokens;
-         n += (int64_t)gridDim.x * (kCombineThreads / kLanes)) {
-        for (int col = part * 8; col < features; col += kLanes * 8) {
-            float sum[8] = {};
-            for (int j = 0; j < top_k; ++j) {
-                const int r = token_row[n * top_k + j];
-                if (r < 0 || r >= n_rows) { bad |= r != -1; continue; }
-                const float w = weight ? weight[n * top_k + j] : 1.f;
-                float v[8];
-                load8(y + (int64_t)r * ld_y, col, features, v);
+    const int64_t step = (int64_t)gridDim.x * (kCombineThreads / kLanes);
+    Slots<kLanes> slots = {token_row, weight, n_tokens, top_k, n_rows};
+    int64_t n = ((int64_t)blockIdx.x * kCombineThreads + threadIdx.x) / kLanes;
+    slots.ask(n, part);
+    for (; __any_sync(kFull, n < n_tokens); n += step) {
+        const int held_r = slots.checked(slots.r);
+        const float held_w = slots.w;
+        slots.ask(n + step, part);
+        for (int col0 = 0; col0 < features; col0 += kLanes * 8 * kBlocks) {
+            const int col = col0 + part * 8;
+            float sum[kBlocks][8] = {};
+            for (int j0 = 0; j0 < top_k; j0 += kSlots) {
+                uint4 q[kSlots][kBlocks];
+                float w[kSlots];
+                int r[kSlots];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+                for (int j = 0; j < kSlots; ++j) {
+                    r[j] = slots.row(n, j0 + j, held_r);
+                    w[j] = slots.factor(n, j0 + j, held_w);
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+                        if (r[j] >= 0 && col + b * kLanes * 8 < features) q[j][b] = load_packed(y + r[j] * ld_y, col + b * kLanes * 8, features);
+                }
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) {
+                    if (r[j] < 0) continue;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[b][i] = fmaf(w[j], to_float(reinterpret_cast<const T *>(&q[j][b])[i]), sum[b][i]);
+                }
             }
-            store8(out + n * ld_out, col, features, sum);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                if (n < n_tokens && col + b * kLanes * 8 < features) store8(out + n * ld_out, col + b * kLanes * 8, features, sum[b]);
         }
     }
-    if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    if (slots.bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
 }
 
+// Eight columns of d_out, packed where they are 16-bit values.
+template <typename T, typename O> struct Gradient {
+    uint4 q;
+    __device__ __forceinline__ void load(const T *row, int col, int features) { q = load_packed(row, col, features); }
+    __device__ __forceinline__ float at(int i) const { return to_float(reinterpret_cast<const T *>(&q)[i]); }
+};
+template <typename T> struct Gradient<T, float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float *row, int col, int features) { load8(row, col, features, v); }
+    __device__ __forceinline__ float at(int i) const { return v[i]; }
+};
+
 template <typename T, typename O, int kLanes>
-__global__ void __launch_bounds__(kCombineThreads)
+__global__ void __launch_bounds__(kCombineThreads, 4)
 combine_backward_kernel(const O *__restrict__ d_out, int64_t ld_d, const T *__restrict__ y, int n_rows, int64_t ld_y,
                         const int32_t *__restrict__ token_row, const float *__restrict__ weight, int64_t n_tokens,
                         int top_k, int features, bool relu, T *__restrict__ dy, int64_t ld_dy,
@@ -92,42 +168,64 @@ combine_backward_kernel(const O *__restrict__ d_out, int64_t ld_d, const T *__re
     dependent_begin();
     const int part = threadIdx.x % kLanes;
     const bool reads_y = d_weight || relu;
-    bool bad = false;
-    // (all lanes of a warp stay in the loop: the sums below are exchanged between a token's lanes)
     const int64_t step = (int64_t)gridDim.x * (kCombineThreads / kLanes);
-    const int64_t n_first = ((int64_t)blockIdx.x * kCombineThreads + threadIdx.x) / kLanes;
-    for (int64_t n = n_first; __any_sync(kFull, n < n_tokens); n += step) {
-        for (int j = 0; j < top_k; ++j) {
-            int r = -1;
-            if (n < n_tokens) {
-                r = token_row[n * top_k + j];
-                if (r < -1 || r >= n_rows) { bad = true; r = -1; }
+    Slots<kLanes> slots = {token_row, weight, n_tokens, top_k, n_rows};
+    int64_t n = ((int64_t)blockIdx.x * kCombineThreads + threadIdx.x) / kLanes;
+    slots.ask(n, part);
+    for (; __any_sync(kFull, n < n_tokens); n += step) {
+        const int held_r = slots.checked(slots.r);
+        const float held_w = slots.w;
+        slots.ask(n + step, part);
+        for (int j0 = 0; j0 < top_k; j0 += kSlots) {
+            int r[kSlots];
+            float w[kSlots], dot[kSlots];
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j) {
+                r[j] = slots.row(n, j0 + j, held_r);
+                w[j] = slots.factor(n, j0 + j, held_w);
+                dot[j] = 0.f;
             }
-            float dot = 0.f;
-            if (r >= 0) {
-                const float w = weight ? weight[n * top_k + j] : 1.f;
-                for (int col = part * 8; col < features; col += kLanes * 8) {
-                    float g[8], v[8];
-                    load8(d_out + n * ld_d, col, features, g);
-                    if (reads_y) load8(y + (int64_t)r * ld_y, col, features, v);
-                    if (d_weight)
+            for (int col = part * 8; n < n_tokens && col < features; col += kLanes * 8 * kBlocks) {
+                uint4 q[kSlots][kBlocks];
+                Gradient<T, O> g[kBlocks];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) dot = fmaf(v[i], g[i], dot);
-                    if (dy) {
+                for (int b = 0; b < kBlocks; ++b) {
+                    const int c = col + b * kLanes * 8;
+                    if (c >= features) continue;
+                    g[b].load(d_out + n * ld_d, c, features);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) g[i] = relu && !(v[i] > 0.f) ? 0.f : w * g[i];
-                        store8(dy + (int64_t)r * ld_dy, col, features, g);
+                    for (int j = 0; j < kSlots; ++j)
+                        if (reads_y && r[j] >= 0) q[j][b] = load_packed(y + r[j] * ld_y, c, features);
+                }
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    const int c = col + b * kLanes * 8;
+                    if (c >= features) continue;
+#pragma unroll
+                    for (int j = 0; j < kSlots; ++j) {
+                        if (r[j] < 0) continue;
+                        float z[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float v = reads_y ? to_float(reinterpret_cast<const T *>(&q[j][b])[i]) : 0.f;
+                            if (d_weight) dot[j] = fmaf(v, g[b].at(i), dot[j]);
+                            z[i] = relu && !(v > 0.f) ? 0.f : w[j] * g[b].at(i);
+                        }
+                        if (dy) store8(dy + r[j] * ld_dy, c, features, z);
                     }
                 }
             }
             if (d_weight) {
 #pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(kFull, dot, o);
-                if (part == 0 && n < n_tokens) d_weight[n * top_k + j] = dot;
+                for (int j = 0; j < kSlots; ++j) {
+#pragma unroll
+                    for (int o = kLanes / 2; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(kFull, dot[j], o);
+                    if (part == 0 && n < n_tokens && j0 + j < top_k) d_weight[n * top_k + j0 + j] = dot[j];
+                }
             }
         }
     }
-    if (bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
+    if (slots.bad) atomicOr(status, (unsigned)GS_DEV_BAD_VALUE);
 }
 
 template <typename F> cudaError_t by_lanes(int features, F &&f) {
@@ -139,7 +237,7 @@ template <typename F> cudaError_t by_lanes(int features, F &&f) {
 
 int combine_ctas(const gs_ctx *ctx, int64_t n_tokens, int lanes) {
     const int64_t want = (n_tokens * lanes + kCombineThreads - 1) / kCombineThreads;
-    const int64_t most = (int64_t)ctx->n_sm * 32;
+        const int64_t most = (int64_t)ctx->n_sm * 4;     // as many as are resident (launch bounds)
     return (int)(want < most ? want : most);
 }
 
