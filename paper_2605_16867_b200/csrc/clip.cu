@@ -64,7 +64,7 @@ __device__ __forceinline__ int to_boundary(const T *p, int n) {
 
 template <typename T>
 __device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
-    constexpr int kN = Pack<T>::kN, kAhead = 4;
+    constexpr int kN = Pack<T>::kN, kAhead = 2;      // (16 bytes each; at 268 M elements 1 / 2 / 3 / 4 / 8 of them take 360 / 300 / 325 / 415 / 655 us)
     const int head = to_boundary(g, n), packs = (n - head) / kN, tail = head + packs * kN;
     const uint4 *q = reinterpret_cast<const uint4 *>(g + head);
     double sum = 0.0;
@@ -83,7 +83,7 @@ __device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T *g, T *out, int n, float f) {
-    constexpr int kN = Pack<T>::kN, kAhead = 4;
+    constexpr int kN = Pack<T>::kN, kAhead = 2;      // (16 bytes each; at 268 M elements 1 / 2 / 3 / 4 / 8 of them take 360 / 300 / 325 / 415 / 655 us)
     if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
         for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(to_float(g[i]) * f);
         return;
@@ -119,7 +119,7 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 template <int kMost>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 2)
 norm_kernel(const __grid_constant__ ClipTable<kMost> t, double *__restrict__ partials)
 {
     dependent_begin();
@@ -151,7 +151,7 @@ __device__ __forceinline__ float clip_factor(const double *__restrict__ partials
 }
 
 template <int kMost>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 2)
 clip_kernel(const __grid_constant__ ClipTable<kMost> t, const double *__restrict__ partials, int n_partials, float max_norm,
             float *__restrict__ out_norm, unsigned *__restrict__ status)
 {
@@ -176,7 +176,7 @@ cudaError_t launch_tables(gs_ctx *ctx, const gs_grad *grads, int n_tensors, floa
     double *partials = operator_scratch(ctx).clip_partials;
     const int n_tables = n_tensors > kMost ? (n_tensors + kMost - 1) / kMost : 1;
     int per_table = kMaxClipCtas / n_tables;
-    if (per_table > ctx->n_sm * 4) per_table = ctx->n_sm * 4;
+    if (per_table > ctx->n_sm * 2) per_table = ctx->n_sm * 2;        // as many as are resident
     if (per_table < 1) return cudaErrorInvalidValue;
     int n_partials = 0;
     for (int pass = 0; pass < 2; ++pass) {

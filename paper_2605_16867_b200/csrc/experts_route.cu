@@ -577,6 +577,85 @@ route_place_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_
         row_token[i] = -1;
 }
 
+// The same for few experts, without any exchange between lanes: every thread takes a run of
+// consecutive slots of a block in shared memory (an odd number: no bank conflicts), counts them in a column of its own; the columns' prefix sums per expert are the threads' first rows.  The rows of the CTAs
+// before this one are added up here as well (n_experts * gridDim.x numbers), which saves a launch.
+constexpr int kRun = 7, kRunSlots = kRun * kRouteThreads;
+__global__ void __launch_bounds__(kRouteThreads)
+route_place_runs_kernel(const int32_t *__restrict__ expert, int64_t n_slots, int top_k, int slots_per_cta, int n_experts,
+                        const int *__restrict__ counts, int32_t *__restrict__ offsets, int32_t *__restrict__ row_token,
+                        int32_t *__restrict__ token_row)
+{
+    __shared__ int slot_row[kRunSlots];              // a block of slots: their experts, then their rows
+    extern __shared__ int place_smem[];
+    int *total = place_smem, *next = total + n_experts, *start = next + n_experts, *cnt = start + n_experts + 1;
+    dependent_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t cta_first = min((int64_t)blockIdx.x * slots_per_cta, n_slots), cta_last = min(cta_first + slots_per_cta, n_slots);
+    for (int e = warp; e < n_experts; e += kRouteThreads / 32) {
+        int all = 0, early = 0;
+        for (int c = lane; c < (int)gridDim.x; c += 32) {
+            const int v = counts[e * kMaxRouteCtas + c];
+            all += v;
+            early += c < (int)blockIdx.x ? v : 0;
+        }
+        all = __reduce_add_sync(kFull, all);
+        early = __reduce_add_sync(kFull, early);
+        if (lane == 0) { total[e] = all; next[e] = early; }
+    }
+    __syncthreads();
+    if (warp == 0) prefix_experts(n_experts, lane, start, [&](int e) { return total[e]; });
+    __syncthreads();
+    for (int e = threadIdx.x; e < n_experts; e += kRouteThreads) next[e] += start[e];
+    int *mine = cnt + threadIdx.x;                   // [n_experts][kRouteThreads]
+    for (int64_t block = cta_first; block < cta_last; block += kRunSlots) {
+        const int n = (int)min((int64_t)kRunSlots, cta_last - block);
+        for (int i = threadIdx.x; i < kRunSlots; i += kRouteThreads) slot_row[i] = i < n ? expert[block + i] : -1;
+        for (int e = 0; e < n_experts; ++e) mine[e * kRouteThreads] = 0;
+        __syncthreads();
+        int *run = slot_row + threadIdx.x * kRun;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) if (run[i] >= 0) mine[run[i] * kRouteThreads] += 1;
+        __syncthreads();
+        for (int e = warp; e < n_experts; e += kRouteThreads / 32) {
+            int row = next[e];
+            for (int base = 0; base < kRouteThreads; base += 32) {
+                const int own = cnt[e * kRouteThreads + base + lane];
+                int sum = own;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(kFull, sum, o);
+                    if (lane >= o) sum += up;
+                }
+                cnt[e * kRouteThreads + base + lane] = row + sum - own;
+                row += __shfl_sync(kFull, sum, 31);
+            }
+            if (lane == 0) next[e] = row;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const int e = run[i];
+            if (e < 0) continue;
+            const int row = mine[e * kRouteThreads];
+            mine[e * kRouteThreads] = row + 1;
+            run[i] = row;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += kRouteThreads) {
+            const int row = slot_row[i];
+            token_row[block + i] = row;
+            if (row >= 0) row_token[row] = (int)((unsigned)(block + i) / (unsigned)top_k);
+        }
+        __syncthreads();
+    }
+    if (blockIdx.x == 0)
+        for (int e = threadIdx.x; e <= n_experts; e += kRouteThreads) offsets[e] = start[e];
+    const int64_t step = (int64_t)gridDim.x * kRouteThreads;
+    for (int64_t i = start[n_experts] + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; i < n_slots; i += step)
+        row_token[i] = -1;
+}
+
 // Few tokens: choice and order in one launch of one CTA.
 constexpr int kSmallThreads = 512;
 template <typename T, int V, bool kTokens>
@@ -804,6 +883,13 @@ template <typename T> cudaError_t route_as(gs_ctx *ctx, const ExpertRouteArgs &a
     }
     if (e != cudaSuccess || !counts) return e;
     const int warps = kRouteThreads / 32;
+    if (tokens) {
+        const size_t smem = sizeof(int) * ((size_t)kRouteThreads * p.n_experts + 3 * p.n_experts + 1);
+        LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
+        return launch_dependent(route_place_runs_kernel, dim3(n_ctas), dim3(kRouteThreads), smem, st, (const int32_t *)a.expert,
+                                a.n_tokens * p.top_k, p.top_k, rows_per_cta * p.top_k, p.n_experts,
+                                (const int *)counts, a.offsets, a.row_token, a.token_row);
+    }
     {
         LaunchTimer t(ctx, GS_K_EXPERT_ROUTE, st);
         e = launch_dependent(route_prefix_kernel, dim3((p.n_experts + warps - 1) / warps), dim3(kRouteThreads), 0, st,
