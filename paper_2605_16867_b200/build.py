@@ -1,11 +1,11 @@
 """Builds libgoodserve.so (hand-written CUDA for sm_100a) in-tree with nvcc."""
 from __future__ import annotations
 
+import hashlib
 import os
 import shutil
 import subprocess
 import sys
-import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -17,6 +17,9 @@ COUNT_LIB_PATH = os.path.join(_PKG, "libgoodserve_count.so")    # the measuring 
 DEBUG_LIB_PATH = os.path.join(_PKG, "libgoodserve_debug.so")    # the checking build (-DGS_DEBUG)
 SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu", "operators_api.cu", "experts_route.cu",
            "experts_linear.cu", "experts_combine.cu", "clip.cu")
+MACRO_SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu")    # what -DGS_COUNT_EVALS and -DGS_DEBUG reach
+OBJ_DIR = os.path.join(_PKG, "_build")
+_compiled = set()                                               # objects that this process has built
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-cudart", "shared")
 
@@ -43,22 +46,25 @@ def build_library(force: bool = False, verbose: bool = False, extra_flags=(), co
     path = COUNT_LIB_PATH if counting else DEBUG_LIB_PATH if checking else LIB_PATH
     if not force and not _stale(path):
         return path
-    if counting:
-        extra_flags = (*extra_flags, "-DGS_COUNT_EVALS")
-    elif checking:
-        extra_flags = (*extra_flags, "-DGS_DEBUG")
-    # one compiler process per source file, side by side, then one link
-    with tempfile.TemporaryDirectory(prefix="goodserve_build_") as objects:
-        def compile_one(source: str) -> str:
-            obj = os.path.join(objects, source + ".o")
-            cmd = [_nvcc(), *NVCC_FLAGS, *extra_flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", obj]
-            if verbose:
-                print(" ".join(cmd), file=sys.stderr)
-            subprocess.run(cmd, check=True)
+    macros = ("-DGS_COUNT_EVALS",) if counting else ("-DGS_DEBUG",) if checking else ()
+    # one compiler process per source file, side by side, then one link; the sources that neither of the
+    # two macros reaches are compiled once for all three builds
+    def compile_one(source: str) -> str:
+        flags = (*NVCC_FLAGS, *extra_flags, *(macros if source in MACRO_SOURCES else ()))
+        obj = os.path.join(OBJ_DIR, f"{hashlib.sha1(' '.join(flags).encode()).hexdigest()[:12]}_{source}.o")
+        if obj in _compiled or not (force or _stale(obj)):
             return obj
-        with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as workers:
-            built = list(workers.map(compile_one, SOURCES))
-        subprocess.run([_nvcc(), *NVCC_FLAGS, "--shared", *built, "-o", path + ".tmp"], check=True)
+        cmd = [_nvcc(), *flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", f"{obj}.{os.getpid()}"]
+        if verbose:
+            print(" ".join(cmd), file=sys.stderr)
+        subprocess.run(cmd, check=True)
+        os.replace(f"{obj}.{os.getpid()}", obj)
+        _compiled.add(obj)
+        return obj
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as workers:
+        built = list(workers.map(compile_one, SOURCES))
+    subprocess.run([_nvcc(), *NVCC_FLAGS, "--shared", *built, "-o", path + ".tmp"], check=True)
     os.replace(path + ".tmp", path)
     return path
 
