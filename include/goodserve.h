@@ -42,7 +42,8 @@
  *     [0, n_instances) is clamped into range; a bit of the device status word records it
  *     (gs_device_status).  A NaN deadline is never met, so such a request takes the fallback.
  *   - Calls of the same kind on one context must not overlap on the GPU (they share the
- *     context's scratch memory).  gs_route_batch / gs_advance_state on one stream and
+ *     context's scratch memory: so do gs_expert_route calls, and gs_clip_grad_norm calls;
+ *     products and combinations have none).  gs_route_batch / gs_advance_state on one stream and
  *     gs_risk_scan on another may overlap each other: they use separate scratch.
  */
 #ifndef GOODSERVE_H_
@@ -82,8 +83,8 @@ enum gs_dev_status {
     GS_DEV_BAD_TYPE = 2,        /* type_id outside [0, n_types) was read as 0 */
     GS_DEV_BAD_VALUE = 4,       /* negative count or negative/NaN q_ema was read as 0; NaN score; index of a row or an
                                    expert outside its range; global gradient norm that is not finite */
-    GS_DEV_TIMEOUT = 8,         /* a bounded device-side wait expired (the route kernel's wait for its table
-                                   copies); the outputs of that call are invalid */
+    GS_DEV_TIMEOUT = 8,         /* a bounded device-side wait expired (the route kernel's wait for its table copies, or
+                                   one between the parts of an expert product); the outputs of that call are invalid */
     GS_DEV_CAND_TRUNCATED = 16, /* more flagged requests than cand_capacity; list was cut */
     GS_DEV_INTERNAL = 32        /* only from a library built with -DGS_DEBUG: one of its index checks failed
                                    (a table index computed by the search fell outside its table) */
@@ -602,8 +603,8 @@ typedef struct gs_grad {
 /*
  * Global norm over all tensors, norm = sqrt(sum of squares), and clipping by it:
  *   out = grad * f,  f = min(1, max_norm / (norm + 1e-6))   computed in float, rounded once.
- * `grads` is a HOST array (read before the call returns).  Squares and their sum are in double, so
- * neither the largest nor the smallest gradients are lost, and the sum's order is fixed.
+ * `grads` is a HOST array (read before the call returns).  The sum is in double, and so are squares that
+ * a float cannot hold, so neither the largest nor the smallest gradients are lost; its order is fixed.
  * *out_norm: one float on the device.  A norm that is not finite leaves the values as they are
  * (f = 1) and sets GS_DEV_BAD_VALUE; max_norm >= 0 (not NaN), +infinity never clips.  With `out`
  * NULL in every entry only the norm is computed.

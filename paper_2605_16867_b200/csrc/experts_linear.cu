@@ -2,16 +2,22 @@
 //   forward   y[r]  = act(x[t(r)] W_e^T + b_e)         per row r of expert e
 //   backward  dx[r] = dz[r] W_e  (zero where x[t(r)] <= 0),   dW_e = sum_r dz[r]^T x[t(r)],   db_e = sum_r dz[r]
 //
-// Every kernel is persistent: one pair of CTAs per pair of SMs takes tiles in turn.  Six or seven
-// warps have fixed parts: warp 0 copies operand tiles into a ring of shared-memory stages, warp 1 of
-// the leader issues the matrix instructions, warps 2-5 move finished sums from tensor memory to
-// global memory while the next tile is already being summed (two sets of sums in tensor memory).
-// Which rows belong to which expert is read from the offsets on the device; the host knows only
-// their number.
+// Every kernel is persistent: one pair of CTAs per pair of SMs takes tiles in turn, and its warps have
+// fixed parts: warp 0 copies operand tiles into a ring of shared-memory stages (with gathered rows
+// others issue the gathers), warp 1 of the leader issues the matrix instructions, four or eight move
+// finished sums from tensor memory to global memory while the next tile is already being summed
+// (two sets of sums in tensor memory).  Which rows belong to which expert is read from the offsets
+// on the device; the host knows only their number.
 //
 // In y and dx the tile's 256 "M" rows are weights (features of the result), its "N" columns are
 // requests: few rows per expert then cost little (N can be small, the weights are read once), and
-// with many rows a pair reads 64 KB per 64 of the contraction for 256 x 256 results.
+// with many rows a pair reads 64 KB per 64 of the contraction for 256 x 256 results.  Bound by the
+// matrix instructions: 65,536 rows each twice, 2048 to 1024, read in order, take 390-410 us = 1.34-1.41
+// PFLOP/s, 80-84 % of a library product's burst and 94-99 % of its sustained rate on the same card (the
+// clock falls to some 1.45 GHz under this load; 669 cycles per step of 64 where the instructions need 512).
+// Waiting on barriers with cluster-wide acquire and release cost half of that speed (695 TFLOP/s): the
+// waits and arrivals below therefore order the CTA alone, and the one that follows plain writes to
+// shared memory has its own fence.
 #include <type_traits>
 
 #include "operators.cuh"
@@ -26,7 +32,7 @@ constexpr int kDepth = 64;                      // of the contraction per stage:
 constexpr int kHalfM = 128;                     // rows of the result per CTA of a pair
 constexpr int kTileM = 2 * kHalfM;
 constexpr uint32_t kABytes = kHalfM * 128;
-constexpr int kWarpProducer = 0, kWarpMma = 1;      // the next four (eight in dW) store, dW's last one clears
+constexpr int kWarpProducer = 0, kWarpMma = 1;
 constexpr int kMaxStages = 10;
 // A gather instruction fetches four rows, one lane at a time; one warp issues them in some 75 cycles
 // each, far below what the copies could carry.  131,072 requests of the first layer with 1 / 4 / 8 /
@@ -348,10 +354,17 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 // the workspace and a second launch adds them in order.  The tensor cores cut off what does not fit
 // a sum (they do not round), so a long chain of additions drifts towards zero: 2e-6 of the result
 // after 2,048 rows.  A chain therefore ends after kChain steps, and the storing warps add the
-// chains' sums, rounding, in registers (eight warps, half a result row each) while the next chain runs.  Rows past the expert's last one are those
-// of the next expert (or anything at all): warp 6 clears them in shared memory before the matrix
-// instructions may read them.  db is one more product, with a block of ones, for the tiles of the
-// first in features.
+// chains' sums, rounding, in registers (eight warps, half a result row each) while the next chain
+// runs.  (65,536 requests, first layer: off by 4.8e-7 of the result with chains of 8 steps, 7.3e-7 with
+// 12; where every pair has one tile, chains of 8 / 16 / 32 steps and no chains take 635 / 597 / 575 / 562 us.)
+//
+// Rows past the expert's last one are those of the next expert (or anything at all): warp 2 clears
+// them in shared memory before the matrix instructions may read them.  db is one more product, with a
+// block of ones, for the tiles of the first in features.
+//
+// Cutting (pieces per pair 1 / 2 / 3 / 4, at least 32 steps each): one expert, 16,384 rows, 2368 x 2048
+// 303 / 251 / 230 / 238 us; nine experts, 65,536 requests twice 693 / 688 / 638 / 641 us.  Pieces of at least 32 / 64
+// steps: nine experts, 65,536 requests of 512 to 256 129 / 85 us, sixteen of 256 to 256 48 / 58 us.
 
 constexpr int kMinPiece = 48;                   // steps of 64 rows; an expert is not cut finer
 constexpr int kPiecesPerPair = 3;
@@ -794,12 +807,16 @@ bool encode_weights(CUtensorMap *map, const ExpertLinearArgs &a, int box_rows) {
 
 int pairs_of(const gs_ctx *ctx) { return ctx->n_sm / 2; }
 
-// Calls f with the width of the N tile: the widest that the average expert fills well.
+// Calls f with the width of the N tile, by the average expert's rows.  A step of 64 takes some 0.35 us
+// whatever the width (the weights' 128 rows per CTA bound it), so a tile that covers most experts whole
+// is best, and a wider one only adds copies.  2048 to 1024, nine experts, widths 32 / 64 / 128 / 256:
+// 57 rows each 26 / 16 / 17 / 20 us, 133 rows 38 / 27 / 18 / 25 us, 266 rows 60 / 39 / 29 / 21 us;
+// 512 to 512, 64 experts: 15 rows 11.5 / 11.8 / 12.3 / 13.7 us, 62 rows 20 / 15 / 14 / 16 us, 156 rows 36 / 24 / 20 / 20 us.
 template <typename F> cudaError_t by_rows(const ExpertLinearArgs &a, F &&f) {
     const int64_t each = a.n_rows / a.n_experts;
-    if (each >= 160) return f(std::integral_constant<int, 256>());
-    if (each >= 80) return f(std::integral_constant<int, 128>());
-    if (each >= 40) return f(std::integral_constant<int, 64>());
+    if (each >= 140) return f(std::integral_constant<int, 256>());
+    if (each >= 60) return f(std::integral_constant<int, 128>());
+    if (each >= 24) return f(std::integral_constant<int, 64>());
     return f(std::integral_constant<int, 32>());
 }
 

@@ -6,9 +6,14 @@
 //
 // A choice is a comparison of floats, so it is made on order-preserving 32-bit keys (key 0: not to
 // be chosen) with the lowest index winning among equal keys.  The order of the rows is a counting
-// sort by expert in three launches that share one partition of the tokens into runs, one per CTA:
-// count (in the routing kernel), prefix sums, place.  No atomics on floats, nothing that depends
-// on the order of execution.
+// sort by expert in launches that share one partition of the tokens into runs, one per CTA: count (in
+// the routing kernel), prefix sums (with few experts part of the next), place.  No atomics on
+// floats, nothing that depends on the order of execution.
+//
+// Bound by instruction issue (a row is 36 to 512 bytes of logits and some hundred instructions), hence
+// one thread per row with few experts (1,048,576 x 9, top 2: 23 us of routing, 385 instructions per 32
+// rows, and 16 us of placing; a warp per row took 630 us) and one warp per row with many
+// (131,072 x 256 in groups: 117 us, 707 instructions a row; its gradient 61 us).
 #include <type_traits>
 
 #include "operators.cuh"
