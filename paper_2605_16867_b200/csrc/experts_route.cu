@@ -74,35 +74,36 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 1 / (1 + exp(-x)); the reciprocal is the approximate one (1 ulp).  0 at -infinity.
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + exp2_fast(-kLog2e * x)); }
 
-// A row's logits, experts lane * V .. lane * V + V - 1; -infinity where there is none.
-// `whole`: rows start so aligned, and experts divide so evenly, that a lane's can be read at once.
-// True if one of them is infinite or not a number (or there is none): the caller then cleans them.
-template <typename T, int V>
-__device__ __forceinline__ bool load_row(const T *__restrict__ row, int n_experts, int lane, bool whole, float (&x)[V]) {
-    const int first = lane * V;
+// A lane's part of a row, experts lane * V .. lane * V + V - 1, as it lies in memory: the next row's is
+// asked for while this one is worked on.  `whole`: rows start so aligned, and experts divide so evenly,
+// that it can be read at once.
+template <typename T, int V> struct RawRow {
+    alignas(16) T v[V];
+    __device__ __forceinline__ void load(const T *__restrict__ row, int n_experts, int lane, bool whole) {
+        const int first = lane * V;
+        if (whole) {
+            constexpr int kBytes = V * sizeof(T) < 16 ? V * sizeof(T) : 16;
+            using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, unsigned, unsigned short>>>;
+            if (first < n_experts) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = -INFINITY;
-    if (whole) {
-        constexpr int kBytes = V * sizeof(T) < 16 ? V * sizeof(T) : 16, kEach = kBytes / sizeof(T);
-        using Word = std::conditional_t<kBytes == 16, uint4, std::conditional_t<kBytes == 8, uint2, std::conditional_t<kBytes == 4, unsigned, unsigned short>>>;
-        if (first < n_experts) {
-#pragma unroll
-            for (int w = 0; w < V / kEach; ++w) {
-                const Word q = __ldg(reinterpret_cast<const Word *>(row + first) + w);
-                const T *t = reinterpret_cast<const T *>(&q);
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) x[w * kEach + i] = to_float(t[i]);
+                for (int w = 0; w < V * (int)sizeof(T) / kBytes; ++w) reinterpret_cast<Word *>(v)[w] = __ldg(reinterpret_cast<const Word *>(row + first) + w);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (first + i < n_experts) v[i] = row[first + i];
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) if (first + i < n_experts) x[i] = to_float(row[first + i]);
     }
-    float odd = 0.f;                                 // 0 * x is not a number for either
+    // -infinity where there is none.  True if one is infinite or not a number (or there is none): the caller then cleans them.
+    __device__ __forceinline__ bool unpack(int n_experts, int lane, float (&x)[V]) const {
+        float odd = 0.f;                             // 0 * x is not a number for either
 #pragma unroll
-    for (int i = 0; i < V; ++i) odd = fmaf(x[i], 0.f, odd);
-    return odd != odd;
-}
+        for (int i = 0; i < V; ++i) {
+            x[i] = lane * V + i < n_experts ? to_float(v[i]) : -INFINITY;
+            odd = fmaf(x[i], 0.f, odd);
+        }
+        return odd != odd;
+    }
+};
 
 template <int V> __device__ __forceinline__ void clean_row(float (&x)[V], bool *nan) {
 #pragma unroll
@@ -271,10 +272,15 @@ __device__ __forceinline__ void route_rows(const T *__restrict__ logits, int64_t
     int lanes = 0;
     if (p.n_groups > 1 && p.group_size % V == 0 && (p.group_size / V & (p.group_size / V - 1)) == 0) lanes = p.group_size / V;
     const bool halved = V > 1 && lanes && p.top_groups * p.group_size <= 16 * V;
-    for (int64_t n = first + warp; n < last; n += blockDim.x >> 5) {
+    const int step = blockDim.x >> 5;
+    RawRow<T, V> raw;
+    if (first + warp < last) raw.load(logits + (first + warp) * ld, p.n_experts, lane, whole);
+    for (int64_t n = first + warp; n < last; n += step) {
         float s[V];
         unsigned key[V], off = 0;
-        if (load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s)) {
+        const bool odd = raw.unpack(p.n_experts, lane, s);
+        if (n + step < last) raw.load(logits + (n + step) * ld, p.n_experts, lane, whole);
+        if (odd) {
             clean_row<V>(s, &nan);
 #pragma unroll
             for (int i = 0; i < V; ++i) off |= (s[i] == -INFINITY ? 1u : 0u) << i;
@@ -718,12 +724,23 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float *mine = row_smem[warp];
     bool bad = false;
-    for (int64_t n = (int64_t)blockIdx.x * kWarps + warp; n < n_tokens; n += (int64_t)gridDim.x * kWarps) {
+    const int64_t step = (int64_t)gridDim.x * kWarps;
+    RawRow<T, V> raw;
+    int next_expert = -1;
+    float next_dw = 0.f;
+    const auto ask = [&](int64_t n) {
+        if (n >= n_tokens) return;
+        raw.load(logits + n * ld, p.n_experts, lane, whole);
+        if (lane < p.top_k) { next_expert = expert[n * p.top_k + lane]; next_dw = d_weight[n * p.top_k + lane]; }
+    };
+    ask((int64_t)blockIdx.x * kWarps + warp);
+    for (int64_t n = (int64_t)blockIdx.x * kWarps + warp; n < n_tokens; n += step) {
         float s[V];
-        if (load_row<T, V>(logits + n * ld, p.n_experts, lane, whole, s)) clean_row<V>(s, &bad);
-        int e = lane < p.top_k ? expert[n * p.top_k + lane] : -1;
+        if (raw.unpack(p.n_experts, lane, s)) clean_row<V>(s, &bad);
+        int e = next_expert;
         if (e < -1 || e >= p.n_experts) { bad = true; e = -1; }
-        const float dw = e >= 0 ? d_weight[n * p.top_k + lane] : 0.f;
+        const float dw = e >= 0 ? next_dw : 0.f;
+        ask(n + step);
         scores_of<V>(s, p.sigmoid);
 #pragma unroll
         for (int i = 0; i < V; ++i) mine[lane * V + i] = s[i];
