@@ -13,6 +13,7 @@ namespace gs {
 namespace tc {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
+constexpr unsigned kSuspendNs = 1000000u;            // how long one try may sleep (it wakes up when the phase completes)
 constexpr long long kWaitLimit = 8000000000ll;       // cycles (four seconds or more): a wait that takes this long has failed
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -50,8 +51,8 @@ __device__ __forceinline__ void bar_arrive_release(uint32_t cluster_bar) {
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\t"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(kSuspendNs) : "memory");
     return ok != 0;
 }
 // Waits for the phase of the given parity.  False: this wait, or another of the CTA, took too long
