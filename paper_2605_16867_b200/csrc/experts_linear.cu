@@ -922,11 +922,15 @@ cudaError_t configure_expert_linear() {
 }
 
 // An expert is cut only if it has more steps than kMinPiece and than a share (the whole work over
-// kPiecesPerPair pieces per pair); it then has at most 2 * steps / share pieces, and all cut
-// experts together at most twice the number of shares.
-int64_t expert_linear_workspace(const gs_ctx *ctx, int, int64_t n_rows, int in, int) {
+// kPiecesPerPair pieces per pair); it then has at most 2 * steps / most pieces of either, and all cut
+// experts together at most twice the number of shares, and twice all steps over kMinPiece (no two
+// experts share a row, whatever the offsets say).
+int64_t expert_linear_workspace(const gs_ctx *ctx, int n_experts, int64_t n_rows, int in, int out) {
     if (n_rows <= kMinPiece * kDepth) return 0;
-    return 2 * (int64_t)pairs_of(ctx) * kPiecesPerPair * (kTileM * weights_tile(in) + kTileM) * 4;
+    const int kn = weights_tile(in);
+    const int64_t tiles = (int64_t)((in + kn - 1) / kn) * ((out + kTileM - 1) / kTileM);
+    const int64_t by_share = 2 * (int64_t)pairs_of(ctx) * kPiecesPerPair, by_steps = 2 * tiles * (n_rows / kDepth + n_experts) / kMinPiece + 1;
+    return (by_share < by_steps ? by_share : by_steps) * (kTileM * kn + kTileM) * 4;
 }
 
 cudaError_t launch_expert_linear(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st) {
