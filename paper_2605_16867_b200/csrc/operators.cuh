@@ -68,7 +68,6 @@ __device__ __forceinline__ void dependent_begin() {
 __device__ __forceinline__ void dependent_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dependent_end() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-
 // Launches a kernel once the one before it has ended (no programmatic dependence).
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_after(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
