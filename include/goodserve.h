@@ -472,6 +472,7 @@ enum gs_dtype { GS_F32 = 0, GS_BF16 = 1, GS_F16 = 2 };
 #define GS_MAX_TOP_K 16
 #define GS_MAX_EXPERT_GROUPS 32
 #define GS_MAX_FEATURES (1 << 20)
+#define GS_MAX_EXPERT_ROWS (2147483647 - 512)   /* rows of one product: its row indices are 32-bit and run up to two tiles past the last row */
 
 enum gs_expert_score { GS_SCORE_SOFTMAX = 0, GS_SCORE_SIGMOID = 1 };
 
@@ -535,6 +536,7 @@ GS_API int gs_expert_route_backward(gs_ctx *ctx, const void *logits, int logits_
  *   x           [n_x_rows, in_features]       w  [n_experts, out_features, in_features] (rows ld_w apart,
  *   bias        float [n_experts, out_features] or NULL      experts out_features * ld_w apart)
  *   offsets     int32 [n_experts + 1] on the device, as gs_expert_route leaves them
+ *   n_rows      0 .. GS_MAX_EXPERT_ROWS
  *   out         [n_rows, out_features]; rows past offsets[n_experts] are not written
  * Without row_token n_x_rows must be n_rows.  Offsets are clamped into [0, n_rows]; a row_token
  * outside [0, n_x_rows) is clamped into it and sets GS_DEV_BAD_VALUE.

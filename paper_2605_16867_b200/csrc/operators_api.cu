@@ -47,7 +47,7 @@ int check_linear(const gs_ctx *ctx, const gs::ExpertLinearArgs &a) {
     if (!ctx || !is_operand(a.dtype)) return GS_ERR_INVALID_ARG;
     if (a.n_experts < 1 || a.n_experts > GS_MAX_EXPERTS) return GS_ERR_INVALID_ARG;
     if (a.in < 1 || a.in > GS_MAX_FEATURES || a.out < 1 || a.out > GS_MAX_FEATURES) return GS_ERR_INVALID_ARG;
-    if (a.n_rows < 0 || a.n_rows > kMaxRows || a.n_x_rows < 0 || a.n_x_rows > kMaxRows) return GS_ERR_INVALID_ARG;
+    if (a.n_rows < 0 || a.n_rows > GS_MAX_EXPERT_ROWS || a.n_x_rows < 0 || a.n_x_rows > kMaxRows) return GS_ERR_INVALID_ARG;
     if (!a.row_token && a.n_x_rows != a.n_rows) return GS_ERR_INVALID_ARG;
     if (a.row_token && a.n_rows > 0 && a.n_x_rows < 1) return GS_ERR_INVALID_ARG;
     GS_TRY(check_array(a.offsets, false));
@@ -130,7 +130,7 @@ GS_API int gs_expert_linear(gs_ctx *ctx, int dtype, const void *x, int64_t n_x_r
 GS_API int64_t gs_expert_linear_backward_workspace(const gs_ctx *ctx, int32_t n_experts, int64_t n_rows,
                     int32_t in_features, int32_t out_features)
 {
-    if (!ctx || n_experts < 1 || n_experts > GS_MAX_EXPERTS || n_rows < 0 || n_rows > kMaxRows || in_features < 1 ||
+    if (!ctx || n_experts < 1 || n_experts > GS_MAX_EXPERTS || n_rows < 0 || n_rows > GS_MAX_EXPERT_ROWS || in_features < 1 ||
         in_features > GS_MAX_FEATURES || out_features < 1 || out_features > GS_MAX_FEATURES)
         return GS_ERR_INVALID_ARG;
     return gs::expert_linear_workspace(ctx, n_experts, n_rows, in_features, out_features);

@@ -1,0 +1,46 @@
+"""CPU-only checks of the length predictor's operators: what the C entry points refuse before they touch
+the device, and the build of their sources.
+
+A refused call returns before the context is used, so a zeroed block of memory stands for one."""
+import ctypes as C
+
+import pytest
+
+INVALID, ALIGN = -1, -4
+I32_MAX = 2 ** 31 - 1
+MOST_ROWS = I32_MAX - 512
+GOOD, ODD = 4096, 4104                          # addresses that no call reads: aligned, not aligned
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2605_16867_b200.binding import load_library
+    return load_library()
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    block = C.create_string_buffer(1 << 16)
+    yield C.addressof(block)
+
+
+def linear(lib, ctx, n_rows, x, n_x_rows=None, row_token=None):
+    return lib.gs_expert_linear(ctx, 1, x, n_rows if n_x_rows is None else n_x_rows, 64, row_token, GOOD, 1, n_rows, GOOD, 64, None, 64, 64, 0,
+                                GOOD, 64, None)
+
+
+def linear_backward(lib, ctx, n_rows, dz):
+    return lib.gs_expert_linear_backward(ctx, 1, dz, 64, GOOD, n_rows, 64, None, GOOD, 1, n_rows, GOOD, 64, 64, 64, 0, GOOD, 64, None, 0, None,
+                                         None, 0, None)
+
+
+def test_products_refuse_rows_that_their_indices_cannot_reach(lib, ctx):
+    # A tile of 256 rows that begins inside the last expert ends, and is rounded up, up to two tiles past its
+    # end; all of that is 32-bit arithmetic.  (The unaligned address is looked at after the number of rows.)
+    assert linear(lib, ctx, MOST_ROWS, ODD) == ALIGN
+    assert linear_backward(lib, ctx, MOST_ROWS, ODD) == ALIGN
+    for rows in (MOST_ROWS + 1, I32_MAX - 255, I32_MAX - 1, I32_MAX, I32_MAX + 1):
+        assert linear(lib, ctx, rows, ODD) == INVALID
+        assert linear(lib, ctx, rows, ODD, n_x_rows=5, row_token=GOOD) == INVALID
+        assert linear_backward(lib, ctx, rows, ODD) == INVALID
+        assert lib.gs_expert_linear_backward_workspace(ctx, 1, rows, 64, 64) == INVALID
