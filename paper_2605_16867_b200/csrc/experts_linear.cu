@@ -37,7 +37,7 @@ constexpr int kMaxStages = 10;
 // A gather instruction fetches four rows, one lane at a time; one warp issues them in some 75 cycles
 // each, far below what the copies could carry.  131,072 requests of the first layer with 1 / 4 / 8 /
 // 16 warps: 2,160 / 970 / 889 / 877 us.
-constexpr int kGatherWarps = 8;
+constexpr int kGatherWarps = 8;                 // (at most: four rows each are the least)
 
 struct Barriers {
     uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], sums_full[2], sums_empty[2];
@@ -135,7 +135,12 @@ template <int kN> struct RowsShape {
     static constexpr int kStoreBytes = kStoreWarps * 2048;   // per warp: 32 requests x 32 features
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + sizeof(Barriers) + (3 * GS_MAX_EXPERTS + 4) * sizeof(int);
     static constexpr int kTmem = 2 * kN < 32 ? 32 : 2 * kN;
-    static constexpr int threads(bool gather) { return 32 * (2 + kStoreWarps + (gather ? kGatherWarps - 1 : 0)); }
+    // Every gathering warp has rows: one without would follow the ring's barriers for nothing, and since no copy
+    // of its own holds a stage back, could fall a round behind and then wait for a phase that never comes.
+    static constexpr int kGatherers = kN / 8 < kGatherWarps ? kN / 8 : kGatherWarps;
+    static constexpr int kGatherLanes = kN / (8 * kGatherers);                      // of each of them: four rows per lane
+    static_assert(kGatherLanes >= 1 && kGatherers * kGatherLanes * 4 == kN / 2, "a gathering warp without rows");
+    static constexpr int threads(bool gather) { return 32 * (2 + kStoreWarps + (gather ? kGatherers - 1 : 0)); }
 };
 
 // kDx: the weights' tile has its features contiguous (the contraction runs over their rows).
@@ -169,7 +174,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
     const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
     if (warp == kWarpProducer || warp >= 2 + S::kStoreWarps) {
-        const int helper = warp == kWarpProducer ? 0 : warp - (1 + S::kStoreWarps);     // kGatherWarps warps share out the gathered rows
+        const int helper = warp == kWarpProducer ? 0 : warp - (1 + S::kStoreWarps);     // the gathering warps share out the rows
         if (threadIdx.x == 0) { prefetch_map(&map_w); prefetch_map(&map_x); }
         Ring ring;
         int e = 0;
@@ -178,10 +183,9 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             const int rt = (int)(t / m_tiles), m0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM;
             while (tile_start[e + 1] <= rt) ++e;
             const int r0 = row_start[e] + (rt - tile_start[e]) * kN + (int)rank * (kN / 2);
-            constexpr int kLanes = kN >= 8 * kGatherWarps ? kN / (8 * kGatherWarps) : 1;     // of each warp: four rows per lane
-            const int row = (helper * kLanes + lane) * 4;
+            const int row = (helper * S::kGatherLanes + lane) * 4;
             int token[4];
-            if (kGather && lane < kLanes && row < kN / 2) {
+            if (kGather && lane < S::kGatherLanes) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     token[i] = safe_token(p.row_token[min(r0 + row + i, row_end[e] - 1)], p.n_tokens, &bad);
@@ -200,7 +204,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                     }
                     if (!kGather) copy_2d(&map_x, b, full, k * kDepth, r0);
                 }
-                if (kGather && lane < kLanes && row < kN / 2) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
+                if (kGather && lane < S::kGatherLanes) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
                 __syncwarp();
                 ring.next(S::kStages);
             }
@@ -401,6 +405,7 @@ template <int kN> struct WeightsShape {
     static constexpr int kOnesBytes = 2048;
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreBytes + kOnesBytes + sizeof(Barriers) + sizeof(Pieces);
     static constexpr int kTmem = 2 * kN;
+    static_assert(kGatherWarpsDw <= 16 * (kN / 128), "a gathering warp without rows");
     static constexpr int kPartial = kTileM * kN + kTileM;    // floats of one piece: sums, then db
 };
 

@@ -1,0 +1,69 @@
+"""The experts' products where a pair of thread blocks works on several tiles, one after the other: the ring of
+operand stages, the two sets of sums and the experts' rows carry over from tile to tile.
+
+Tolerances as in test_gpu_operators.py: (n + 8) * 2^-23 times the sum of the magnitudes of a dot product's n
+terms, then one rounding to the output's type."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_operators import BF16, F16, UNIT, clean_status, close, gen, gs, layout, normal, of_rows, padded, rest, segments  # noqa: E402, F401
+
+
+def uneven(experts, rows, g):
+    """Rows of every expert, adding up to `rows`: some far above the mean, some none, some one."""
+    share = torch.rand(experts, generator=g, device="cuda").pow(2) + 0.05
+    counts = (share / share.sum() * (rows - experts)).long()
+    counts[1::7], counts[2::11] = 0, 1
+    counts[0] += rows - counts.sum()
+    return counts.tolist()
+
+
+# experts, rows, in, out: the average expert's rows choose the tile's width; at least three tiles for each of 74 pairs
+# in both directions
+TILES = [
+    (300, 4100, 400, 1100),                     # 32 wide
+]
+
+
+def tiles_id(c):
+    return f"{c[0]}e-{c[1]}r-{c[2]}-{c[3]}"
+
+
+def inputs(case, gather, dtype):
+    experts, rows, i, o = case
+    g = gen(rows)
+    counts = uneven(experts, rows, g)
+    offsets, rows, row_token = layout(counts, g, rows // 2 if gather else None)
+    x = normal(rows // 2 if gather else rows, i, dtype, g, extra=1)
+    w = padded(experts * o, i, dtype)
+    w.copy_(torch.randn(experts * o, i, generator=g, device="cuda") * i ** -0.5)
+    return g, offsets, rows, row_token, x, w.unflatten(0, (experts, o)), torch.randn(experts, o, generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("case", TILES, ids=tiles_id)
+@pytest.mark.parametrize("gather", [False, True], ids=["in-order", "gathered"])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_rows_over_several_tiles_of_a_pair(gs, case, gather, dtype):  # noqa: F811
+    experts, _, i, o = case
+    g, offsets, rows, row_token, x, w, bias = inputs(case, gather, dtype)
+    dz = normal(rows, o, dtype, g)
+    out, dx = padded(rows, o, dtype, extra=1), padded(rows, i, dtype, extra=1)
+    gs.expert_linear(x, w, offsets, out, bias=bias, row_token=row_token, relu=True)
+    gs.expert_linear_backward(dz, x, w, offsets, dx=dx, row_token=row_token, relu_input=True)
+    xs, zs = of_rows(x, row_token).double(), dz.double()
+    for e, r in segments(offsets):
+        we = w[e].double()
+        want = (xs[r] @ we.T + bias[e].double()).clamp_min(0)
+        mag = xs[r].abs() @ we.abs().T + bias[e].double().abs()
+        close(out[r], want, (i + 8) * 2.0 ** -23 * mag + UNIT[dtype] * want.abs() + 2.0 ** -25)
+        want = torch.where(xs[r] > 0, zs[r] @ we, 0.0)
+        close(dx[r], want, (o + 8) * 2.0 ** -23 * (zs[r].abs() @ we.abs()) + UNIT[dtype] * want.abs() + 2.0 ** -25)
+    assert torch.isnan(rest(out)).all() and torch.isnan(rest(dx)).all()
+    for _ in range(5):                          # the same every time, and no wait ran out
+        again, back = padded(rows, o, dtype), padded(rows, i, dtype)
+        gs.expert_linear(x, w, offsets, again, bias=bias, row_token=row_token, relu=True)
+        gs.expert_linear_backward(dz, x, w, offsets, dx=back, row_token=row_token, relu_input=True)
+        assert torch.equal(again, out) and torch.equal(back, dx)
+    assert gs.device_status() == 0
