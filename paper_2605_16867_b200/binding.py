@@ -589,9 +589,10 @@ class GoodServe:
             dwp, lddw = _stack(dw, torch.float32, w.shape, "dw", dev)
             need = self._lib.gs_expert_linear_backward_workspace(self._h, e, rows, i, o)
             if need > 0:
-                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-                if stream is not None:
-                    workspace.record_stream(stream)
+                # (from the pool of the stream that uses it: what another stream gave back there, that stream's
+                # kernels may still be writing)
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
         self._check(self._lib.gs_expert_linear_backward(
             self._h, _DTYPES[dt], zp, ldz, xp, nx, ldx, _array(row_token, torch.int32, rows, "row_token", dev),
             _array(offsets, torch.int32, e + 1, "offsets", dev), e, rows, wp, ldw, i, o, 2 if relu_input else 0,

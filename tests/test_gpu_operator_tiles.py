@@ -67,3 +67,63 @@ def test_rows_over_several_tiles_of_a_pair(gs, case, gather, dtype):  # noqa: F8
         gs.expert_linear_backward(dz, x, w, offsets, dx=back, row_token=row_token, relu_input=True)
         assert torch.equal(again, out) and torch.equal(back, dx)
     assert gs.device_status() == 0
+
+
+def cut_inputs(case, gather, dtype):
+    """Experts with more rows than one piece holds, by their rows: their sums pass through the workspace."""
+    counts, i, o = case
+    g = gen(i + o)
+    offsets, rows, row_token = layout(counts, g, sum(counts) // 2 if gather else None)
+    x = normal(rows // 2 if gather else rows, i, dtype, g)
+    w = padded(len(counts) * o, i, dtype, 0.0).unflatten(0, (len(counts), o))
+    return offsets, rows, row_token, x, w, normal(rows, o, dtype, g)
+
+
+def weight_buffers(case):
+    counts, i, o = case
+    return (torch.full((len(counts), o, (i + 3) // 4 * 4 + 4), float("nan"), device="cuda")[..., :i],
+            torch.full((len(counts), o), float("nan"), device="cuda"))
+
+
+def test_workspace_belongs_to_the_stream_that_uses_it(gs, monkeypatch):  # noqa: F811
+    case = ([9001, 0, 4097, 63], 263, 515)
+    offsets, rows, _, x, w, dz = cut_inputs(case, False, BF16)
+    side, taken = torch.cuda.Stream(), []
+    empty = torch.empty
+
+    def recorded(*args, **kwargs):
+        taken.append((torch.cuda.current_stream().cuda_stream, kwargs.get("device")))
+        return empty(*args, **kwargs)
+    dw, db = weight_buffers(case)
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch, "empty", recorded)
+    gs.expert_linear_backward(dz, x, w, offsets, dw=dw, db=db)
+    gs.expert_linear_backward(dz, x, w, offsets, dw=dw, db=db, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    gs.expert_linear_backward(dz, x, w, offsets, dw=dw, db=db, stream=side)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    here = torch.cuda.current_stream().cuda_stream
+    assert [s for s, _ in taken] == [here, here, side.cuda_stream]
+
+
+def test_gradients_on_two_streams_at_once(gs):  # noqa: F811
+    """One gradient after the other on the current and a side stream, nothing waited for: as one by one."""
+    case = ([9001, 0, 4097, 63], 263, 515)
+    offsets, rows, _, x, w, dz = cut_inputs(case, False, BF16)
+    other = normal(rows, case[2], BF16, gen(2))
+    want = [weight_buffers(case) for _ in range(2)]
+    for d, (dw, db) in zip((dz, other), want):
+        gs.expert_linear_backward(d, x, w, offsets, dw=dw, db=db)
+        torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = [[weight_buffers(case) for _ in range(10)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        gs.expert_linear_backward(dz, x, w, offsets, dw=a[0], db=a[1])
+        gs.expert_linear_backward(other, x, w, offsets, dw=b[0], db=b[1], stream=side)
+    torch.cuda.synchronize()
+    for mine, ref in zip(got, want):
+        for dw, db in mine:
+            assert torch.equal(dw, ref[0]) and torch.equal(db, ref[1])
+    assert gs.device_status() == 0
