@@ -434,10 +434,11 @@ __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n
         total += score;
         if (j == 0) q0 = score; else if (j == 1) q1 = score; else weights[j] = score;
     }
-    const float f = p.renormalise ? __fdividef(p.scale, total) : p.scale;
-    weights[0] = f * q0;
-    if (p.top_k > 1) weights[1] = f * q1;
-    for (int j = 2; j < p.top_k; ++j) weights[j] = f * weights[j];
+    // (the score is divided first: scale / total alone can leave the range of a float)
+    const auto weigh = [&](float q) { return p.scale * (p.renormalise ? __fdividef(q, total) : q); };
+    weights[0] = weigh(q0);
+    if (p.top_k > 1) weights[1] = weigh(q1);
+    for (int j = 2; j < p.top_k; ++j) weights[j] = weigh(weights[j]);
 }
 
 template <typename T, int E, bool kBias>
