@@ -61,18 +61,22 @@ __device__ __forceinline__ float clean_logit(float v, bool *nan) {
     return fminf(v, kLargest);
 }
 
-// 2^y by the special function unit (2^-22 relative).  exp(x) = 2^(x log2 e): rounding the exponent
-// costs |x| * 2^-24, so a score of e^-10 is good to some 2^-20; the larger ones, which are chosen, to 2^-22.
-// (The library's exponential takes four times the instructions, and instructions bound these kernels.)
-__device__ __forceinline__ float exp2_fast(float y) {
+// 1 / v to one unit in the last place, v in [1, 2].
+__device__ __forceinline__ float reciprocal(float v) {
     float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-constexpr float kLog2e = 1.4426950408889634f;
 
-// 1 / (1 + exp(-x)); the reciprocal is the approximate one (1 ulp).  0 at -infinity.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + exp2_fast(-kLog2e * x)); }
+// 1 / (1 + exp(-x)), by the exponential that cannot overflow: e^x / (1 + e^x) below zero.  0 at -infinity.
+// (Exponentials here and below are the library's: 2 units, and what a float can hold below 2^-126 too, so
+// that scores far below the best one keep their order.  2^y of the special function unit with y = x log2 e
+// rounded is off by |x| 2^-24 more and ends at 2^-126; it saves 4 us of 39 at 1,048,576 x 9 and 12 us of 201
+// at 131,072 x 256 with the gradient.)
+__device__ __forceinline__ float sigmoid(float x) {
+    const float e = expf(-fabsf(x)), r = reciprocal(1.f + e);
+    return x < 0.f ? e * r : r;
+}
 
 // A lane's part of a row, experts lane * V .. lane * V + V - 1, as it lies in memory: the next row's is
 // asked for while this one is worked on.  `whole`: rows start so aligned, and experts divide so evenly,
@@ -129,7 +133,7 @@ __device__ __forceinline__ void scores_of(float (&x)[V], bool sigmoid_score) {
     top = fmaxf(warp_max(top), -kLargest);           // (nothing left: every exponential is 0)
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) { x[i] = exp2_fast((x[i] - top) * kLog2e); sum += x[i]; }
+    for (int i = 0; i < V; ++i) { x[i] = expf(x[i] - top); sum += x[i]; }
     sum = warp_sum(sum);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
@@ -330,7 +334,7 @@ __device__ __forceinline__ void route_rows(const T *__restrict__ logits, int64_t
         const float total = warp_sum(my_score) + kSumFloor;
         if (lane < p.top_k) {
             out_expert[n * p.top_k + lane] = my_expert;
-            out_weight[n * p.top_k + lane] = p.scale * (p.renormalise ? __fdividef(my_score, total) : my_score);
+            out_weight[n * p.top_k + lane] = p.scale * (p.renormalise ? my_score / total : my_score);
             if (cta_count && my_expert >= 0) atomicAdd(&cta_count[my_expert], 1);
         }
         __syncwarp();
@@ -383,7 +387,7 @@ __device__ __forceinline__ float token_scores_once(const float (&x)[E], float (&
 #pragma unroll
     for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
 #pragma unroll
-    for (int e = 0; e < E; ++e) { s[e] = exp2_fast((x[e] - top) * kLog2e); sum += s[e]; }
+    for (int e = 0; e < E; ++e) { s[e] = expf(x[e] - top); sum += s[e]; }
     return sum;
 }
 // NaNs and +infinity make the sum a NaN; only then the logits are looked at one by one.
@@ -434,8 +438,9 @@ __device__ __forceinline__ void route_token(const T *__restrict__ row, int64_t n
         total += score;
         if (j == 0) q0 = score; else if (j == 1) q1 = score; else weights[j] = score;
     }
-    // (the score is divided first: scale / total alone can leave the range of a float)
-    const auto weigh = [&](float q) { return p.scale * (p.renormalise ? __fdividef(q, total) : q); };
+    // (the scale comes last: scale / total alone can leave the range of a float)
+    const float share = p.renormalise ? 1.f / total : 1.f;
+    const auto weigh = [&](float q) { return p.scale * (q * share); };
     weights[0] = weigh(q0);
     if (p.top_k > 1) weights[1] = weigh(q1);
     for (int j = 2; j < p.top_k; ++j) weights[j] = weigh(weights[j]);

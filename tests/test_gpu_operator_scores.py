@@ -36,3 +36,47 @@ def test_weights_of_any_scale(gs, experts, n, scale):  # noqa: F811
         assert (weight[expert < 0] == 0).all() and (expert[::3] == -1).all()
         close(weight, unit[1].double() * scale, 2.0 ** -22 * abs(scale) * unit[1].double())
     assert gs.device_status() == 0
+
+
+def exact_scores(x, score):
+    x = x.double()
+    return torch.sigmoid(x) if score == "sigmoid" else torch.softmax(x, 1)
+
+
+@pytest.mark.parametrize("experts", [9, 16, 32, 40, 200])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+def test_scores_far_below_the_best(gs, experts, score, dtype):  # noqa: F811
+    """Every score of rows whose logits spread over a hundred and more, in steps that all types hold exactly."""
+    k = min(16, experts)
+    for n in (60, 4000):
+        g = gen(experts + n)
+        x = (torch.randint(-240, 200, (n, experts), generator=g, device="cuda").float() / 4).to(dtype)
+        expert, weight, *_ = route(gs, x, router_of(experts, k, score=score, renormalise=False))
+        s = exact_scores(x, score)
+        want = s.gather(1, expert.long())
+        close(weight, want, 2.0 ** -18 * want + 2 * LEAST)
+        if experts <= 16 and score == "softmax":             # all of them were chosen, the largest first (sigmoids meet at one)
+            held = s.float()
+            order = torch.sort(torch.where(held >= 4 * LEAST, held, 0.0), dim=1, descending=True, stable=True)[1]
+            clear = (torch.sort(held, dim=1, descending=True)[0][:, :k] >= 4 * LEAST)
+            assert torch.equal(expert[clear].long(), order[:, :k][clear])
+        # weights of a dense choice add up to one
+        _, weight, *_ = route(gs, x, router_of(experts, k, score=score))
+        total = want.sum(1, keepdim=True) + 1e-20
+        close(weight, want / total, 2.0 ** -18 * want / total + 4 * LEAST / total.clamp_max(1.0))
+    assert gs.device_status() == 0
+
+
+@pytest.mark.parametrize("experts,groups", [(9, 1), (40, 1), (64, 8)])
+def test_choice_below_the_least_normal_score(gs, experts, groups):  # noqa: F811
+    """One expert takes all but e^-88 and less; the next places go by what is left, not by the index."""
+    for n in (50, 4000):
+        x = torch.full((n, experts), -200.0, device="cuda")
+        x[:, 5], x[:, 3], x[:, 6], x[:, 1] = 0.0, -95.0, -90.0, -99.0
+        router = router_of(experts, 4, n_groups=groups, top_groups=groups)
+        expert, weight, *_ = route(gs, x, router)
+        assert expert.unique(dim=0).tolist() == [[5, 6, 3, 1]]
+        want = torch.tensor([0.0, -90.0, -95.0, -99.0], device="cuda").double().exp().expand(n, 4)
+        close(weight, want, 2.0 ** -18 * want + 4 * LEAST)
+    assert gs.device_status() == 0
