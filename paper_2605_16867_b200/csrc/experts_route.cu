@@ -78,6 +78,12 @@ __device__ __forceinline__ float sigmoid(float x) {
     return x < 0.f ? e * r : r;
 }
 
+// Its slope s (1 - s) = e^-|x| / (1 + e^-|x|)^2, without the difference, which has no digits left from x = 17 on.
+__device__ __forceinline__ float sigmoid_slope(float x) {
+    const float e = expf(-fabsf(x)), r = reciprocal(1.f + e);
+    return e * r * r;
+}
+
 // A lane's part of a row, experts lane * V .. lane * V + V - 1, as it lies in memory: the next row's is
 // asked for while this one is worked on.  `whole`: rows start so aligned, and experts divide so evenly,
 // that it can be read at once.
@@ -717,7 +723,7 @@ route_small_kernel(const T *__restrict__ logits, int n_tokens, int64_t ld, bool 
 
 // Gradient of the weights, one warp per row.  With q the chosen scores, t = sum q + 1e-20:
 //   renormalised: dq_j = scale * (dw_j - sum_i dw_i q_i / t) / t;   else dq_j = scale * dw_j
-//   sigmoid: dx = dq * s (1 - s);   softmax: dx = s * (dq - sum_j dq_j s_j)
+//   sigmoid: dx = dq * s (1 - s), by the logit;   softmax: dx = s * (dq - sum_j dq_j s_j)
 template <typename T, int V>
 __global__ void __launch_bounds__(kRouteThreads)
 route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64_t ld, bool whole, RouterParams p,
@@ -747,9 +753,14 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
         if (e < -1 || e >= p.n_experts) { bad = true; e = -1; }
         const float dw = e >= 0 ? next_dw : 0.f;
         ask(n + step);
-        scores_of<V>(s, p.sigmoid);
+        if (p.sigmoid) {                             // the scores to shared memory, their slopes in s
 #pragma unroll
-        for (int i = 0; i < V; ++i) mine[lane * V + i] = s[i];
+            for (int i = 0; i < V; ++i) { mine[lane * V + i] = sigmoid(s[i]); s[i] = sigmoid_slope(s[i]); }
+        } else {
+            scores_of<V>(s, false);
+#pragma unroll
+            for (int i = 0; i < V; ++i) mine[lane * V + i] = s[i];
+        }
         __syncwarp();
         const float q = e >= 0 ? mine[e] : 0.f;      // lane j: the score of slot j
         __syncwarp();
@@ -768,7 +779,7 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float ds = mine[lane * V + i];
-            dx[i] = p.sigmoid ? ds * s[i] * (1.f - s[i]) : s[i] * (ds - mean);
+            dx[i] = p.sigmoid ? ds * s[i] : s[i] * (ds - mean);
         }
         __syncwarp();
         T *out = d_logits + n * ld_d + lane * V;
@@ -830,7 +841,7 @@ route_tokens_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int
         for (int e = 0; e < E; ++e) { ds[e] *= p.scale; across += ds[e] * s[e]; }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float dx = p.sigmoid ? ds[e] * s[e] * (1.f - s[e]) : s[e] * (ds[e] - across);
+            const float dx = p.sigmoid ? ds[e] * sigmoid_slope(x[e]) : s[e] * (ds[e] - across);
             if (e < p.n_experts) d_logits[n * ld_d + e] = from_float<T>(dx);
         }
     }

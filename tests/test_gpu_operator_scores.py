@@ -80,3 +80,30 @@ def test_choice_below_the_least_normal_score(gs, experts, groups):  # noqa: F811
         want = torch.tensor([0.0, -90.0, -95.0, -99.0], device="cuda").double().exp().expand(n, 4)
         close(weight, want, 2.0 ** -18 * want + 4 * LEAST)
     assert gs.device_status() == 0
+
+
+@pytest.mark.parametrize("experts", [9, 31, 33, 100, 256])
+@pytest.mark.parametrize("renormalise", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+def test_gradient_of_saturated_sigmoids(gs, experts, renormalise, dtype):  # noqa: F811
+    """dx = dq s (1 - s): held to 2^-17 of the sum of dq's terms' magnitudes times s (1 - s), then rounded once."""
+    k = min(8, experts)
+    router = router_of(experts, k, score="sigmoid", renormalise=renormalise)
+    for n in (1, 500):
+        g = gen(experts)
+        x = ((torch.rand(n, experts, generator=g, device="cuda") * 2 - 1) * 25).to(dtype)
+        x[:, 0], x[:, -1] = 18.0, -30.0
+        expert = route(gs, x, router)[0].long()
+        dw = torch.randn(n, k, generator=g, device="cuda")
+        out = torch.empty_like(x)
+        gs.expert_route_backward(x, router, expert.int(), dw, out)
+        s, rest = torch.sigmoid(x.double()), torch.sigmoid(-x.double())
+        q, dwd = s.gather(1, expert), dw.double()
+        t = q.sum(1, keepdim=True) + 1e-20
+        dq = (dwd - (dwd * q).sum(1, keepdim=True) / t) / t if renormalise else dwd
+        room = (dwd.abs() + (dwd.abs() * q).sum(1, keepdim=True) / t) / t if renormalise else dwd.abs()
+        slope = (s * rest).gather(1, expert)
+        want, mag = (torch.zeros_like(s).scatter_add_(1, expert, v * slope) for v in (dq, room))
+        assert (want.abs().amax(1) > 0).all()
+        close(out, want, 2.0 ** -17 * mag + UNIT[dtype] * want.abs() + (2.0 ** -25 if dtype is F16 else 1e-37))
+    assert gs.device_status() == 0
