@@ -553,7 +553,7 @@ GS_API int gs_expert_linear(gs_ctx *ctx, int dtype, const void *x, int64_t n_x_r
  *                   the gradient per ROW (gs_expert_combine without weights adds a token's rows up)
  *   out_dw[e]     = sum over e's rows of dz[r, :]^T x[t, :]  float [n_experts, out_features, in_features]
  *   out_db[e]     = sum over e's rows of dz[r, :]            float [n_experts, out_features]
- * Each output may be NULL (not all); out_db needs out_dw.  Experts without rows get zeros.  w is
+ * Each output may be NULL (not all, unless n_rows is 0); out_db needs out_dw.  Experts without rows get zeros.  w is
  * read for out_dx only, x for out_dw and the ReLU.  Sums do not depend on the order of execution.
  * workspace: device memory of at least gs_expert_linear_backward_workspace bytes, 16-byte aligned
  * (partial sums where an expert's rows are split; may be NULL when that is 0).
@@ -585,7 +585,7 @@ GS_API int gs_expert_combine(gs_ctx *ctx, int dtype, const void *y, int64_t n_ro
  *   out_dy[token_row[n, j], :] = weight[n, j] * d_out[n, :]   (y's dtype; with GS_EXPERT_RELU_INPUT zero
  *                                where y is not positive); rows that no slot names are not written
  *   out_d_weight[n, j] = y[token_row[n, j], :] . d_out[n, :]  float; 0 for a slot of row -1.
- * Either output may be NULL (not both); y is read for out_d_weight and the ReLU only.
+ * Either output may be NULL (not both, unless there are no tokens or no rows); y is read for out_d_weight and the ReLU only.
  */
 GS_API int gs_expert_combine_backward(gs_ctx *ctx, int dtype, int d_out_dtype, const void *d_out, int64_t ld_d_out,
                     const void *y, int64_t n_rows, int64_t ld_y, const int32_t *token_row, const float *weight,

@@ -150,8 +150,9 @@ GS_API int gs_expert_linear_backward(gs_ctx *ctx, int dtype, const void *dz, int
     a.db = out_db; a.workspace = workspace;
     GS_TRY(check_linear(ctx, a));
     if (flags & ~GS_EXPERT_RELU_INPUT) return GS_ERR_INVALID_ARG;
-    if ((!out_dx && !out_dw) || (out_db && !out_dw)) return GS_ERR_INVALID_ARG;
-    const bool empty = n_rows == 0, masked = out_dx && (flags & GS_EXPERT_RELU_INPUT);
+    const bool empty = n_rows == 0;                  // (an output without elements may have no address)
+    if ((!out_dx && !out_dw && !empty) || (out_db && !out_dw)) return GS_ERR_INVALID_ARG;
+    const bool masked = out_dx && (flags & GS_EXPERT_RELU_INPUT);
     GS_TRY(check_matrix(dz, ld_dz, out_features, dtype, empty));
     if (out_dw || masked) GS_TRY(check_matrix(x, ld_x, in_features, dtype, empty));
     if (out_dx) {
@@ -204,7 +205,7 @@ GS_API int gs_expert_combine_backward(gs_ctx *ctx, int dtype, int d_out_dtype, c
     if (!ctx || !is_operand(dtype) || (d_out_dtype != dtype && d_out_dtype != GS_F32)) return GS_ERR_INVALID_ARG;
     if (top_k < 1 || top_k > GS_MAX_TOP_K || features < 1 || features > GS_MAX_FEATURES) return GS_ERR_INVALID_ARG;
     if (n_tokens < 0 || n_tokens * (int64_t)top_k > kMaxRows || n_tokens > kMaxRows || n_rows < 0 || n_rows > kMaxRows) return GS_ERR_INVALID_ARG;
-    if ((flags & ~GS_EXPERT_RELU_INPUT) || (!out_dy && !out_d_weight)) return GS_ERR_INVALID_ARG;
+    if ((flags & ~GS_EXPERT_RELU_INPUT) || (!out_dy && !out_d_weight && n_rows > 0 && n_tokens > 0)) return GS_ERR_INVALID_ARG;
     const bool empty = n_tokens == 0, reads_y = out_d_weight || (flags & GS_EXPERT_RELU_INPUT);
     GS_TRY(check_matrix(d_out, ld_d_out, features, d_out_dtype, empty));
     if (reads_y) GS_TRY(check_matrix(y, ld_y, features, dtype, empty || n_rows == 0));

@@ -44,3 +44,18 @@ def test_products_refuse_rows_that_their_indices_cannot_reach(lib, ctx):
         assert linear(lib, ctx, rows, ODD, n_x_rows=5, row_token=GOOD) == INVALID
         assert linear_backward(lib, ctx, rows, ODD) == INVALID
         assert lib.gs_expert_linear_backward_workspace(ctx, 1, rows, 64, 64) == INVALID
+
+
+def test_outputs_without_elements_need_no_address(lib, ctx):
+    # out_dx has n_rows rows, out_dy n_rows, out_d_weight n_tokens: with none of them the tensor's address is null
+    def linear_back(n_rows, dx):
+        return lib.gs_expert_linear_backward(ctx, 1, GOOD, 64, GOOD, n_rows, 64, None, GOOD, 1, n_rows, GOOD, 64, 64, 64, 0, dx, 64, None, 0,
+                                             None, None, 0, None)
+
+    def combine_back(n_rows, n_tokens, dy, d_weight):
+        return lib.gs_expert_combine_backward(ctx, 1, 1, GOOD, 64, GOOD, n_rows, 64, GOOD, None, n_tokens, 2, 64, 0, dy, 64, d_weight, None)
+    assert linear_back(0, None) == 0
+    assert linear_back(1, None) == INVALID
+    assert combine_back(0, 0, None, None) == 0
+    assert combine_back(5, 0, None, None) == 0
+    assert combine_back(5, 1, None, None) == INVALID
