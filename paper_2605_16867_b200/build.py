@@ -19,7 +19,7 @@ SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu", "ope
            "experts_linear.cu", "experts_combine.cu", "clip.cu")
 MACRO_SOURCES = ("api.cu", "prologue.cu", "route.cu", "risk.cu", "sequential.cu")    # what -DGS_COUNT_EVALS and -DGS_DEBUG reach
 OBJ_DIR = os.path.join(_PKG, "_build")
-_compiled = set()                                               # objects that this process has built
+_compiled = set()                                               # objects that this process has built (and, while they are not stale, does not force again)
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-cudart", "shared")
 
@@ -52,7 +52,7 @@ def build_library(force: bool = False, verbose: bool = False, extra_flags=(), co
     def compile_one(source: str) -> str:
         flags = (*NVCC_FLAGS, *extra_flags, *(macros if source in MACRO_SOURCES else ()))
         obj = os.path.join(OBJ_DIR, f"{hashlib.sha1(' '.join(flags).encode()).hexdigest()[:12]}_{source}.o")
-        if obj in _compiled or not (force or _stale(obj)):
+        if not _stale(obj) and (obj in _compiled or not force):
             return obj
         cmd = [_nvcc(), *flags, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, source), "-o", f"{obj}.{os.getpid()}"]
         if verbose:

@@ -59,3 +59,49 @@ def test_outputs_without_elements_need_no_address(lib, ctx):
     assert combine_back(0, 0, None, None) == 0
     assert combine_back(5, 0, None, None) == 0
     assert combine_back(5, 1, None, None) == INVALID
+
+
+def test_build_follows_a_source_that_changes(tmp_path, monkeypatch):
+    """Two builds in one process with an edit between them; a forced one compiles everything once, and what no
+    macro reaches once for all three libraries."""
+    import os
+    import shutil
+    from paper_2605_16867_b200 import build
+    csrc, include, compiled = tmp_path / "csrc", tmp_path / "include", []
+    csrc.mkdir(), include.mkdir()
+    (include / "goodserve.h").write_text("")
+    for name in ("macro.cu", "plain.cu"):
+        (csrc / name).write_text(f"{name} 1\n")
+
+    def stand_in(cmd, check):
+        """Compiles by copying, links by joining."""
+        out = cmd[cmd.index("-o") + 1]
+        if "-c" in cmd:
+            source = cmd[cmd.index("-c") + 1]
+            compiled.append(os.path.basename(source))
+            shutil.copyfile(source, out)
+        else:
+            with open(out, "w") as f:
+                f.write("".join(open(a).read() for a in cmd if a.endswith(".o")))
+    for name, value in dict(CSRC=str(csrc), INCLUDE=str(include), OBJ_DIR=str(tmp_path / "obj"), LIB_PATH=str(tmp_path / "lib.so"),
+                            COUNT_LIB_PATH=str(tmp_path / "count.so"), DEBUG_LIB_PATH=str(tmp_path / "debug.so"), SOURCES=("macro.cu", "plain.cu"),
+                            MACRO_SOURCES=("macro.cu",), _ROOT=str(tmp_path), _compiled=set(), _nvcc=lambda: "nvcc").items():
+        monkeypatch.setattr(build, name, value)
+    monkeypatch.setattr(build.subprocess, "run", stand_in)
+
+    def built(**how):
+        compiled.clear()
+        return open(build.build_library(**how)).read(), sorted(compiled)
+
+    def edit(name, text):
+        (csrc / name).write_text(text)
+        later = max(p.stat().st_mtime for p in tmp_path.rglob("*")) + 5
+        os.utime(csrc / name, (later, later))
+    assert built(force=True) == ("macro.cu 1\nplain.cu 1\n", ["macro.cu", "plain.cu"])
+    assert built(force=True, counting=True) == ("macro.cu 1\nplain.cu 1\n", ["macro.cu"])
+    assert built() == ("macro.cu 1\nplain.cu 1\n", [])
+    edit("plain.cu", "plain.cu 2\n")
+    assert built(force=True)[0] == "macro.cu 1\nplain.cu 2\n"
+    edit("macro.cu", "macro.cu 3\n")
+    assert built()[0] == "macro.cu 3\nplain.cu 2\n"
+    assert built(checking=True)[0] == "macro.cu 3\nplain.cu 2\n"
