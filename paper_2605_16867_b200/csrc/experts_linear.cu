@@ -183,9 +183,12 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
             const int rt = (int)(t / m_tiles), m0 = (int)(t % m_tiles) * kTileM + (int)rank * kHalfM;
             while (tile_start[e + 1] <= rt) ++e;
             const int r0 = row_start[e] + (rt - tile_start[e]) * kN + (int)rank * (kN / 2);
-            const int row = (helper * S::kGatherLanes + lane) * 4;
+            // (of the lanes' condition the second half always holds; without it the compiler issues the gathers
+            // more slowly: 131,072 requests of the first layer 1,138 - 1,190 instead of 970 - 1,020 us, same registers)
+            constexpr int kLanes = S::kGatherLanes;          // of each warp: four rows per lane
+            const int row = (helper * kLanes + lane) * 4;
             int token[4];
-            if (kGather && lane < S::kGatherLanes) {
+            if (kGather && lane < kLanes && row < kN / 2) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     token[i] = safe_token(p.row_token[min(r0 + row + i, row_end[e] - 1)], p.n_tokens, &bad);
@@ -204,7 +207,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                     }
                     if (!kGather) copy_2d(&map_x, b, full, k * kDepth, r0);
                 }
-                if (kGather && lane < S::kGatherLanes) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
+                if (kGather && lane < kLanes && row < kN / 2) copy_rows4(&map_x, b + row * 128, full, k * kDepth, token[0], token[1], token[2], token[3]);
                 __syncwarp();
                 ring.next(S::kStages);
             }
