@@ -30,3 +30,24 @@ def test_gradients_without_rows(gs):  # noqa: F811
     gs.expert_combine(none, lost, out)
     assert (d_weight == 0).all() and (out == 0).all()
     assert gs.device_status() == 0
+
+
+@pytest.mark.parametrize("features", [1, 8, 40, 250, 256, 1000, 1024, 2500])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_combine_backward_writes_the_named_rows_alone(gs, features, dtype):  # noqa: F811
+    n, k = 75, 3
+    g = gen(features)
+    rows = n * k + 20
+    token_row = torch.randperm(rows, generator=g, device="cuda")[: n * k].view(n, k).to(torch.int32)
+    token_row[torch.rand(n, k, generator=g, device="cuda") < 0.2] = -1
+    named = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    named[token_row[token_row >= 0].long()] = True
+    y, weight = normal(rows, features, dtype, g), torch.randn(n, k, generator=g, device="cuda")
+    for d_dtype in (dtype, F32):
+        for relu in (False, True):
+            dy = padded(rows, features, dtype, extra=1)
+            gs.expert_combine_backward(normal(n, features, d_dtype, g), y, token_row, dy=dy, weight=weight, relu=relu)
+            assert torch.isfinite(dy[named]).all()
+            assert torch.isnan(dy[~named]).all()
+            assert torch.isnan(rest(dy)).all()
+    assert gs.device_status() == 0

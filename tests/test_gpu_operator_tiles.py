@@ -24,6 +24,9 @@ def uneven(experts, rows, g):
 # in both directions
 TILES = [
     (300, 4100, 400, 1100),                     # 32 wide
+    (150, 6000, 300, 700),                      # 64
+    (90, 9001, 600, 520),                       # 128
+    (9, 20003, 520, 1030),                      # 256
 ]
 
 
@@ -83,6 +86,40 @@ def weight_buffers(case):
     counts, i, o = case
     return (torch.full((len(counts), o, (i + 3) // 4 * 4 + 4), float("nan"), device="cuda")[..., :i],
             torch.full((len(counts), o), float("nan"), device="cuda"))
+
+
+# rows of every expert, in, out: pieces end inside steps of 64 rows, tiles inside the matrix; 263 and 1000 wide take
+# tiles of 256 columns, 100 those of 128
+CUT = [
+    ([9001, 0, 4097, 63], 263, 515),
+    ([9001, 0, 4097, 63], 1000, 515),
+    ([1, 20011, 3073, 0, 3072], 100, 130),
+    ([6145] * 9, 520, 260),
+]
+
+
+@pytest.mark.parametrize("case", CUT, ids=lambda c: f"{max(c[0])}r-{c[1]}-{c[2]}")
+@pytest.mark.parametrize("gather", [False, True], ids=["in-order", "gathered"])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_gradients_of_experts_that_are_cut(gs, case, gather, dtype):  # noqa: F811
+    offsets, rows, row_token, x, w, dz = cut_inputs(case, gather, dtype)
+    dw, db = weight_buffers(case)
+    gs.expert_linear_backward(dz, x, w, offsets, dw=dw, db=db, row_token=row_token)
+    xs, zs = of_rows(x, row_token), dz.double()
+    for e, r in segments(offsets):
+        n, xe, ze = r.stop - r.start, xs[r].double(), zs[r]
+        # a chain ends after 768 rows and the chains are added in float, so the length in the bound is that of a chain
+        # and the number of chains
+        room = (min(n, 768) + n // 768 + 8) * 2.0 ** -23
+        close(dw[e], ze.T @ xe, room * (ze.abs().T @ xe.abs()) + 1e-30)
+        close(db[e], ze.sum(0), room * ze.abs().sum(0) + 1e-30)
+    beside = torch.as_strided(dw, (dw.shape[0] * dw.shape[1], dw.stride(1) - dw.shape[2]), (dw.stride(1), 1), dw.shape[2])
+    assert torch.isnan(beside).all()
+    for with_db in (True, False, True):
+        again = weight_buffers(case)
+        gs.expert_linear_backward(dz, x, w, offsets, dw=again[0], db=again[1] if with_db else None, row_token=row_token)
+        assert torch.equal(again[0], dw) and (not with_db or torch.equal(again[1], db))
+    assert gs.device_status() == 0
 
 
 def test_workspace_belongs_to_the_stream_that_uses_it(gs, monkeypatch):  # noqa: F811
