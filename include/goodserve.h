@@ -517,8 +517,8 @@ GS_API int gs_expert_route(gs_ctx *ctx, const void *logits, int logits_dtype, in
 /*
  * Gradient of gs_expert_route's weights: d_weight float [n_tokens, top_k] to out_d_logits
  * [n_tokens, n_experts] (the logits' dtype, row stride ld_d_logits), for the choice in `expert`.
- * The choice itself has no gradient, nor has the bias.  A slot whose expert is -1 contributes
- * nothing; one outside [-1, n_experts) neither, and sets GS_DEV_BAD_VALUE.
+ * The choice itself has no gradient, nor has the bias.  `expert` is as gs_expert_route leaves it: a row
+ * names an expert once at most.  A slot whose expert is -1 contributes nothing; one outside [-1, n_experts) neither, and sets GS_DEV_BAD_VALUE.
  */
 GS_API int gs_expert_route_backward(gs_ctx *ctx, const void *logits, int logits_dtype, int64_t n_tokens,
                     int64_t ld_logits, const gs_expert_router *router, const int32_t *expert,
@@ -585,6 +585,7 @@ GS_API int gs_expert_combine(gs_ctx *ctx, int dtype, const void *y, int64_t n_ro
  *   out_dy[token_row[n, j], :] = weight[n, j] * d_out[n, :]   (y's dtype; with GS_EXPERT_RELU_INPUT zero
  *                                where y is not positive); rows that no slot names are not written
  *   out_d_weight[n, j] = y[token_row[n, j], :] . d_out[n, :]  float; 0 for a slot of row -1.
+ * One slot at most names a row (gs_expert_route leaves it so): of two, either's values may stay in out_dy.
  * Either output may be NULL (not both, unless there are no tokens or no rows); y is read for out_d_weight and the ReLU only.
  */
 GS_API int gs_expert_combine_backward(gs_ctx *ctx, int dtype, int d_out_dtype, const void *d_out, int64_t ld_d_out,
@@ -605,8 +606,9 @@ typedef struct gs_grad {
 /*
  * Global norm over all tensors, norm = sqrt(sum of squares), and clipping by it:
  *   out = grad * f,  f = min(1, max_norm / (norm + 1e-6))   computed in float, rounded once.
- * `grads` is a HOST array (read before the call returns).  The sum is in double, and so are squares that
- * a float cannot hold, so neither the largest nor the smallest gradients are lost; its order is fixed.
+ * `grads` is a HOST array (read before the call returns).  Squares are added in float over 16 bytes of a tensor at
+ * a time and in double from there on (squares that a float cannot hold in double from the start, so neither
+ * the largest nor the smallest gradients are lost); the order is fixed.
  * *out_norm: one float on the device.  A norm that is not finite leaves the values as they are
  * (f = 1) and sets GS_DEV_BAD_VALUE; max_norm >= 0 (not NaN), +infinity never clips.  With `out`
  * NULL in every entry only the norm is computed.

@@ -1,10 +1,11 @@
 // Global gradient norm over many tensors, and clipping by it.
 //   norm = sqrt(sum g^2);   out = g * min(1, max_norm / (norm + 1e-6))
 // Bound by memory: one read of everything for the norm, one read and one write for the clipping
-// (the read comes from L2 as far as the gradients fit).  The sum is in double, and so are the squares
-// that leave the range of a float (from 1.8e19 up and 1e-23 down); every CTA leaves one partial sum,
-// which the next launch adds in a fixed order, so the norm is the same every time.  268 M elements, most
-// of them in 16 bits (0.55 GB): 300 us for 1.64 GB moved, 5.5 TB/s; in 32 bits 527 us for 3.2 GB, 6.1 TB/s.
+// (the read comes from L2 as far as the gradients fit).  Squares are added in float over 16 bytes (four or
+// eight values: 2^-22 of the norm at most, and roundings to both sides) and in double from there on; where
+// the sum of those few is outside what a float holds well (1e-24 to 1e38), in double from the start.  Every CTA leaves one
+// partial sum, which the next launch adds in a fixed order, so the norm is the same every time.  268 M elements, most
+// of them in 16 bits (0.55 GB): 305 us for 1.64 GB moved, 5.4 TB/s; in 32 bits 527 us for 3.2 GB, 6.1 TB/s.
 #include "operators.cuh"
 
 namespace gs {
@@ -65,7 +66,7 @@ __device__ __forceinline__ int to_boundary(const T *p, int n) {
 
 template <typename T>
 __device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
-    constexpr int kN = Pack<T>::kN, kAhead = 2;      // (16 bytes each; at 268 M elements 1 / 2 / 3 / 4 / 8 of them take 360 / 300 / 325 / 415 / 655 us)
+    constexpr int kN = Pack<T>::kN, kAhead = 2;      // (16 bytes each; at 268 M elements 1 / 2 / 3 / 4 / 8 of them, here and in chunk_scale, take 360 / 300 / 325 / 415 / 655 us)
     const int head = to_boundary(g, n), packs = (n - head) / kN, tail = head + packs * kN;
     const uint4 *q = reinterpret_cast<const uint4 *>(g + head);
     double sum = 0.0;
@@ -84,7 +85,7 @@ __device__ __forceinline__ double chunk_square(const T *__restrict__ g, int n) {
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T *g, T *out, int n, float f) {
-    constexpr int kN = Pack<T>::kN, kAhead = 2;      // (16 bytes each; at 268 M elements 1 / 2 / 3 / 4 / 8 of them take 360 / 300 / 325 / 415 / 655 us)
+    constexpr int kN = Pack<T>::kN, kAhead = 2;
     if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
         for (int i = threadIdx.x; i < n; i += kClipThreads) out[i] = from_float<T>(to_float(g[i]) * f);
         return;

@@ -12,9 +12,10 @@
 // In y and dx the tile's 256 "M" rows are weights (features of the result), its "N" columns are
 // requests: few rows per expert then cost little (N can be small, the weights are read once), and
 // with many rows a pair reads 64 KB per 64 of the contraction for 256 x 256 results.  Bound by the
-// matrix instructions: 65,536 rows each twice, 2048 to 1024, read in order, take 390-410 us = 1.34-1.41
-// PFLOP/s, 80-84 % of a library product's burst and 94-99 % of its sustained rate on the same card (the
-// clock falls to some 1.45 GHz under this load; 669 cycles per step of 64 where the instructions need 512).
+// matrix instructions and the power they take: 65,536 rows each twice, 2048 to 1024, read in order, take 417 us in
+// two passes after a pause = 1.32 PFLOP/s, 78 % of a library product's burst on the same card, and 462 us repeated for
+// seconds = 1.19 PFLOP/s, 83 % of its sustained rate (1,000 W, SM clock 1,207 MHz; gathered 469 and 522 us, 1,440 MHz).
+// 669 cycles per step of 64 where the instructions need 512.
 // Waiting on barriers with cluster-wide acquire and release cost half of that speed (695 TFLOP/s): the
 // waits and arrivals below therefore order the CTA alone, and the one that follows plain writes to
 // shared memory has its own fence.
@@ -35,8 +36,8 @@ constexpr uint32_t kABytes = kHalfM * 128;
 constexpr int kWarpProducer = 0, kWarpMma = 1;
 constexpr int kMaxStages = 10;
 // A gather instruction fetches four rows, one lane at a time; one warp issues them in some 75 cycles
-// each, far below what the copies could carry.  131,072 requests of the first layer with 1 / 4 / 8 /
-// 16 warps: 2,160 / 970 / 889 / 877 us.
+// each, far below what the copies could carry.  131,072 requests of the first layer in short runs with
+// 1 / 4 / 8 / 16 warps: 2,160 / 970 / 889 / 877 us (eight warps at the power limit, 1,425 MHz: 1,035 us).
 constexpr int kGatherWarps = 8;                 // (at most: four rows each are the least)
 
 struct Barriers {

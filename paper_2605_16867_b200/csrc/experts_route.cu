@@ -7,13 +7,16 @@
 // A choice is a comparison of floats, so it is made on order-preserving 32-bit keys (key 0: not to
 // be chosen) with the lowest index winning among equal keys.  The order of the rows is a counting
 // sort by expert in launches that share one partition of the tokens into runs, one per CTA: count (in
-// the routing kernel), prefix sums (with few experts part of the next), place.  No atomics on
-// floats, nothing that depends on the order of execution.
+// the routing kernel), prefix sums (with few experts part of the next), place.  Nothing depends on the
+// order of execution (the one atomic on floats adds to a place that a row names once).
 //
-// Bound by instruction issue (a row is 36 to 512 bytes of logits and some hundred instructions), hence
-// one thread per row with few experts (1,048,576 x 9, top 2: 23 us of routing, 385 instructions per 32
-// rows, and 16 us of placing; a warp per row took 630 us) and one warp per row with many
-// (131,072 x 256 in groups: 117 us, 761 instructions a row; its gradient 50 us).
+// A row is 36 to 512 bytes of logits and hundreds of instructions, hence one thread per row with few experts and
+// one warp per row with many.  One thread: 1,048,576 x 9, top 2, takes 22 us of choice (466 instructions per
+// 32 rows, 61 % of the issue slots: the rest goes to the rows' scalar loads 36 bytes apart and to fixed
+// latencies, with 32 warps per SM) and 17 us of placing (38 % of the slots: shared memory and barriers); its gradient
+// 33 us.  One warp: 131,072 x 256 in groups takes 118 us (832 instructions a row, 80 % of the slots:
+// bound by issue) and 32 us of order; its gradient 54 us (394 instructions, 86 %).  Few experts in groups
+// go to a warp per row too, with most of its lanes empty: 1,048,576 x 8 in two groups takes 418 us, in one 33 us.
 #include <type_traits>
 
 #include "operators.cuh"
@@ -773,7 +776,7 @@ route_rows_backward_kernel(const T *__restrict__ logits, int64_t n_tokens, int64
 #pragma unroll
         for (int i = 0; i < V; ++i) mine[lane * V + i] = 0.f;
         __syncwarp();
-        if (e >= 0) atomicAdd(&mine[e], dq);         // (a row names an expert once)
+        if (e >= 0) atomicAdd(&mine[e], dq);         // (a row names an expert once at most)
         __syncwarp();
         float dx[V];
 #pragma unroll
