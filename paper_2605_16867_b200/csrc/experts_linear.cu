@@ -67,6 +67,15 @@ struct Ring {
     __device__ __forceinline__ void next(int stages) { if (++stage == stages) { stage = 0; round ^= 1; } }
 };
 
+// By the copying warp at its end: every stage that it filled has been given back.  The matrix instructions'
+// arrivals come from the other CTA too, and none may be under way to this one when it leaves.
+__device__ __forceinline__ void wait_for_stages(Barriers *b, int stages, Ring ring, volatile int *failed) {
+    for (int s = 0; s < stages; ++s) {
+        if (!warp_wait(smem_u32(&b->empty[ring.stage]), ring.round ^ 1, failed)) return;
+        ring.next(stages);
+    }
+}
+
 // Rows of expert e = base + lane, for the lanes of one warp (all experts in turn).  Offsets may be
 // anything: they are clamped into [0, n_rows] and made ascending, so that no two experts share a
 // row; `before` carries the end of the last expert.
@@ -213,6 +222,7 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                 ring.next(S::kStages);
             }
         }
+        if (warp == kWarpProducer && ok) wait_for_stages(bars, S::kStages, ring, failed);
         if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     } else if (warp == kWarpMma) {
         if (rank == 0 && lane == 0) {
@@ -589,6 +599,7 @@ weights_kernel(const __grid_constant__ CUtensorMap map_dz, const __grid_constant
                 ring.next(S::kStages);
             }
         }
+        if (warp == kWarpProducer && ok) wait_for_stages(bars, S::kStages, ring, failed);
         if (bad) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     } else if (warp == kWarpMma) {
         if (rank == 0 && lane == 0) {
