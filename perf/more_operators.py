@@ -155,6 +155,8 @@ def _prepare_recurrence(case, g):
     if case["grad"]:
         s["d_out"], s["d_last"] = _normal(rows, f, t, g, 0.05), _normal(n, f, torch.float32, g, 0.05)
         s["dx"], s["d_gate"], s["d_h0"] = _padded(rows, f, t), _padded(rows, f, t), _padded(n, f, torch.float32)
+        if own:
+            s["states"] = _library().gated_scan_states(rows, n, f)
     return s
 
 
@@ -342,9 +344,8 @@ def _own_recurrence(s):
     if not s["case"]["grad"]:
         gs.gated_scan(s["x"], s["gate"], s["offsets"], out=s["out"], h0=s["h0"], last=s["last"])
         return out
-    states = gs.gated_scan_states(s["x"].shape[0], s["h0"].shape[0], s["x"].shape[1])        # from one direction to the other
-    gs.gated_scan(s["x"], s["gate"], s["offsets"], out=s["out"], h0=s["h0"], last=s["last"], states=states)
-    gs.gated_scan_backward(s["x"], s["gate"], s["offsets"], states, s["dx"], s["d_gate"], d_out=s["d_out"],
+    gs.gated_scan(s["x"], s["gate"], s["offsets"], out=s["out"], h0=s["h0"], last=s["last"], states=s["states"])
+    gs.gated_scan_backward(s["x"], s["gate"], s["offsets"], s["states"], s["dx"], s["d_gate"], d_out=s["d_out"],
                            d_last=s["d_last"], d_h0=s["d_h0"])
     return dict(out, dx=s["dx"], d_gate=s["d_gate"], d_h0=s["d_h0"])
 
