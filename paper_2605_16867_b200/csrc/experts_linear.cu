@@ -512,7 +512,10 @@ rows_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
                 __syncwarp();
             }
             if (end <= 0) {                                   // nothing of this tile is the warp's
-                if (kLinear) fetch_first(spot_after);
+                if constexpr (kLinear) {
+                    fetch_wait<0>();                          // (the zeros that were sent to these places for it land first)
+                    fetch_first(spot_after);
+                }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(in_leader(smem_u32(&bars->sums_empty[use & 1])));
