@@ -176,6 +176,10 @@ __device__ __forceinline__ void cluster_exchange() {     // writes to the other 
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Whether a wait has run out.  The kernel then goes through the turns that are left, as the CTA's barriers want it to, each wait
+// ending with its first try; but a barrier whose phase has not ended takes no further arrival, so nothing more is asked for.
+__device__ __forceinline__ bool failed_yet(const int *failed) { return *(const volatile int *)failed; }
+
 constexpr int kSkip = 3;
 
 // kWarps of a CTA take kBlock rows each in a turn.  Forwards 16 rows of 16-bit values: what a turn costs beside its rows (the
@@ -221,6 +225,7 @@ __device__ __forceinline__ float2 state_before(Exchange *x, int turn, int order,
         }
         return h;
     }
+    const bool failed = failed_yet(&x->failed);
     Map before = nothing();
 #pragma unroll 1
     for (int w = -(-order & 3); w < order; w += 4) {
@@ -233,7 +238,7 @@ __device__ __forceinline__ float2 state_before(Exchange *x, int turn, int order,
     // The last warp tells all CTAs its own one's map.  (They have read what the turn before last left there: each has
     // sent its map of the last turn since, and those are here.)
     if (order == kWarps - 1) {
-        if (lane == 0) expect(smem_u32(&x->told[now]), ctas * 32 * sizeof(float4));
+        if (lane == 0 && !failed) expect(smem_u32(&x->told[now]), ctas * 32 * sizeof(float4));
         const float4 all = kept(then(before, m));
         for (int c = 0; c < ctas; ++c) store_remote(in_cta(smem_u32(&x->totals[now][rank][lane]), c), in_cta(smem_u32(&x->told[now]), c), all);
     }
@@ -362,7 +367,7 @@ gated_scan_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             for (int i = 0; i < kBlock; ++i) m = then(m, {a[i], b[i]});
         }
         h = state_before<kWarps>(ex, turn, order, lane, m, carry, ctas, rank);
-        if (threadIdx.x == 0 && turn + S::kStages < turns) copy(stage, row + S::kStages * step);     // (every warp has read this stage)
+        if (threadIdx.x == 0 && turn + S::kStages < turns && !failed_yet(&ex->failed)) copy(stage, row + S::kStages * step);     // (every warp has read this stage)
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         // (blocks that are there whole, most of them: nothing to look at row by row)
         const bool whole = rows == kBlock && whole_strip;

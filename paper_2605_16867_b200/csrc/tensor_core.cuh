@@ -61,9 +61,10 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 #pragma unroll 1
     for (long long start = 0;;) {
 #pragma unroll 1
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < 64; ++i) {
             if (bar_try(bar, parity)) return true;
-        if (*failed) return false;
+            if (*failed) return false;
+        }
         if (start == 0) start = clock64();
         else if (clock64() - start > kWaitLimit) { *failed = 1; return false; }
     }
