@@ -275,18 +275,20 @@ gated_scan_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     }
     for (int i = threadIdx.x; i < 2 * kSkip * 32; i += S::kThreads) ex->maps[i / (kSkip * 32)][i / 32 % kSkip][i % 32] = kept(nothing());
     dependent_wait();
-    __syncthreads();
-    if (ctas > 1) cluster_exchange();
-
     const int strips = (p.features + kColumns - 1) / kColumns, item = blockIdx.x / ctas;
     const int sequence = item / strips, col0 = item % strips * kColumns, col = col0 + lane * 2;
     const int count = max(0, min(2, p.features - col));
-    const Span span(p, sequence);
-    const int begin = span.begin, end = span.end;
-    if (span.bad && threadIdx.x == 0 && col0 == 0) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
+    // The state before the sequence is read ahead of the barriers: whoever writes the one after it, perhaps over the same memory
+    // (out_last may be h0), does so behind them, whichever CTA of the cluster it is.
     const float *start = kBack ? p.d_last : p.h0;
     float2 carry = both(0.f);
     if (start) carry = unpack<float>(load_pair(start + sequence * (kBack ? p.ld_d_last : p.ld_h0) + col, count));
+    __syncthreads();
+    if (ctas > 1) cluster_exchange();
+
+    const Span span(p, sequence);
+    const int begin = span.begin, end = span.end;
+    if (span.bad && threadIdx.x == 0 && col0 == 0) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     if (begin == end) {
         float *to = kBack ? p.d_h0 : p.last;
         if (to && order == 0 && rank == 0) store_pair(to + sequence * (kBack ? p.ld_d_h0 : p.ld_last) + col, count, carry);
