@@ -1114,14 +1114,14 @@ template <typename T, int kN> cudaError_t dw_as(gs_ctx *ctx, const ExpertLinearA
     const int pairs = pairs_of(ctx);
     cudaError_t e;
     {
-        LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
+        LaunchTimer t(ctx, a.timed_as, st);
         e = a.row_token ? launch_dependent(weights_kernel<T, kN, true>, dim3(2 * pairs), dim3(weights_threads(true)), WeightsShape<kN>::kSmem, st, map_dz, map_x, p)
                         : launch_dependent(weights_kernel<T, kN, false>, dim3(2 * pairs), dim3(weights_threads(false)), WeightsShape<kN>::kSmem, st, map_dz, map_x, p);
     }
     if (e != cudaSuccess || expert_linear_workspace(ctx, a.n_experts, a.n_rows, a.in, a.out) == 0) return e;
     // (not as a programmatic dependent: its CTAs would gather on the SMs whose pairs end first and stay
     // there; 16,384 requests of 1024 to 512: 113 instead of 69 us for both launches)
-    LaunchTimer t(ctx, GS_K_EXPERT_LINEAR, st);
+    LaunchTimer t(ctx, a.timed_as, st);
     return launch_after(weights_sum_kernel<kN>, dim3(4 * ctx->n_sm), dim3(256), 0, st, p, pairs);
 }
 
@@ -1208,6 +1208,7 @@ cudaError_t launch_linear_dw(gs_ctx *ctx, const LinearArgs &a, cudaStream_t st) 
     e.ld_dw = a.ld_dw;
     e.db = a.db;
     e.workspace = a.workspace;
+    e.timed_as = GS_K_LINEAR;
     return launch_expert_linear_dw(ctx, e, st);
 }
 

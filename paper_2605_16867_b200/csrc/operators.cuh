@@ -202,6 +202,7 @@ struct ExpertLinearArgs {
     int64_t ld_dw;
     float *db;
     void *workspace;
+    int timed_as = GS_K_EXPERT_LINEAR;          // the kernel that the launches' time is booked under
 };
 cudaError_t configure_expert_linear();
 cudaError_t launch_expert_linear(gs_ctx *ctx, const ExpertLinearArgs &a, cudaStream_t st);
