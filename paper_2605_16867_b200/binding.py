@@ -727,9 +727,11 @@ class GoodServe:
                                                     None if workspace is None else workspace.data_ptr(), need,
                                                     _raw_stream(dev) if stream is None else stream.cuda_stream))
 
-    def gated_scan_states(self, n_rows: int, n_sequences: int, features: int):
-        """An uninitialised buffer for gated_scan's ``states``."""
-        return torch.empty(n_rows // SCAN_BLOCK + n_sequences, (features + 3) // 4 * 4, dtype=torch.float32, device=self.device)[:, :features]
+    def gated_scan_states(self, n_rows: int, n_sequences: int, features: int, stream=None):
+        """An uninitialised buffer for gated_scan's ``states``, from the pool of the stream that the calls run on."""
+        shape = (n_rows // SCAN_BLOCK + n_sequences, (features + 3) // 4 * 4)
+        with torch.cuda.stream(stream):          # (None: the current one)
+            return torch.empty(shape, dtype=torch.float32, device=self.device)[:, :features]
 
     def gated_scan(self, x, gate, offsets, out=None, h0=None, last=None, states=None, stream=None):
         """gs_gated_scan: h = s(gate) * h + (1 - s(gate)) * x down the rows of every sequence.  x, gate and out [rows, features],

@@ -40,3 +40,16 @@ def test_the_last_state_over_the_first(gs, shape, dtype):  # noqa: F811
         gs.gated_scan(x, gate, offsets, out=again, h0=over, last=over)
         assert torch.equal(over, last) and torch.equal(again, out)
     assert gs.device_status() == 0
+
+
+def test_kept_states_come_from_the_pool_of_their_stream(gs):  # noqa: F811
+    """Memory given back by a program on a side stream goes to that stream's next call, not to another stream's."""
+    side = torch.cuda.Stream()
+    states = gs.gated_scan_states(70001, 3, 1003, stream=side)
+    assert states.shape == (70001 // 8 + 3, 1003) and states.dtype is F32 and states.stride() == (1004, 1)
+    at, size = states.data_ptr(), states.shape[0] * 1004
+    del states
+    here = gs.gated_scan_states(70001, 3, 1003)
+    assert here.data_ptr() != at
+    with torch.cuda.stream(side):
+        assert torch.empty(size, device="cuda").data_ptr() == at
