@@ -3,7 +3,6 @@
 The shape goes by the sequences' average length and number: up to two rows a thread per four columns (forwards), up to eight a
 thread per two, up to 64 four warps a sequence, then 8 or 16 warps and, with few sequences, clusters of up to eight thread
 blocks along each of them."""
-import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -12,6 +11,7 @@ pytestmark = pytest.mark.gpu
 from test_gpu_encoder import (BAD_VALUE, BF16, F16, F32, clean_status, close, gen, gs, normal, padded, reference_scan,  # noqa: E402, F401
                               reference_scan_gradient, rounding, scan_inputs)
 
+INF = float("inf")
 # lengths, features
 SHAPES = {
     "a row or two": ([1, 2, 0, 1] * 30, 70),
@@ -130,3 +130,36 @@ def test_offsets_that_make_no_sense_write_nothing_else(gs, offsets, n, dtype):  
         close(of["last"][k:k + 1], want, want_err + rounding(want, F32))
         alone = covered[b:e] == 1
         close(of["out"][b:e][alone], after[alone], (err + rounding(after, dtype))[alone])
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_nothing_observed_in_sixteen_bits(gs, shape, dtype):  # noqa: F811
+    """A gate of +infinity keeps the state whatever x holds there, one of -infinity replaces it but for 2^-125 of it; a column
+    with a NaN among its gates has no say in the others."""
+    lengths, features = SHAPES[shape]
+    n, s = sum(lengths), len(lengths)
+    x, gate, offsets, h0 = scan_inputs(lengths, features, dtype, 200 + features)
+    g = gen(10)
+    kind = torch.rand(n, features, generator=g, device="cuda")
+    missing, fresh = kind < 0.3, (kind > 0.3) & (kind < 0.4)
+    gate[missing], gate[fresh] = INF, -INF
+    x[missing] = torch.where(torch.rand(n, features, generator=g, device="cuda") < 0.5, float("nan"), INF).to(dtype)[missing]
+    for k in range(1, features, 11):              # (a column of its own each)
+        gate[n // 2, k], x[n // 2, k] = float("nan"), 1.0
+    sound = [k for k in range(features) if k % 11 != 1]
+    out, last, states = padded(n, features, dtype), padded(s, features, F32), gs.gated_scan_states(n, s, features)
+    gs.gated_scan(x, gate, offsets, out=out, h0=h0, last=last, states=states)
+    d_out, d_last = normal(n, features, dtype, g), normal(s, features, F32, g)
+    dx, d_gate, d_h0 = padded(n, features, dtype), padded(n, features, dtype), padded(s, features, F32)
+    gs.gated_scan_backward(x, gate, offsets, states, dx=dx, d_gate=d_gate, d_out=d_out, d_last=d_last, d_h0=d_h0)
+    assert torch.isnan(out[n // 2, 1::11]).all()
+    x, gate, h0, d_out, d_last, missing = (t[:, sound] for t in (x, gate, h0, d_out, d_last, missing))
+    before, after, a, c, err, want, want_err = reference_scan(x, gate, lengths, h0)
+    close(out[:, sound], after, err + rounding(after, dtype))
+    close(last[:, sound], want, want_err + rounding(want, F32))
+    want = reference_scan_gradient(torch.where(missing, 0.0, x), lengths, before, a, c, err, d_out, d_last)
+    close(dx[:, sound], want[0], want[3] + rounding(want[0], dtype))
+    close(d_gate[:, sound], want[1], want[4] + rounding(want[1], dtype) + 2.0 ** -115)
+    close(d_h0[:, sound], want[2], want[5] + rounding(want[2], F32) + 2.0 ** -115)
+    assert (dx[:, sound][missing] == 0).all() and (d_gate[:, sound][missing] == 0).all()
