@@ -42,7 +42,11 @@ template <typename T> __device__ __forceinline__ typename Pair<T>::Raw packed(fl
     if constexpr (std::is_same<T, float>::value) return v;
     else return pack2<T>(v.x, v.y);
 }
-// (count: columns that are there, 2, 1 or none)
+// Columns of a pair that are there, 2, 1 or none, where `left` follow from its first one on.  (A sum of comparisons: a number
+// held to 0 .. 2 by max and min and then compared with 2 under another condition, as `i < rows` of an unrolled loop is, nvcc
+// 12.9.86 compiles wrongly for sm_100a.  Row 1 of a block was not written then, or written past the last column; a kernel of
+// twenty lines does it too.)
+__device__ __forceinline__ int pair_count(int left) { return (left > 0) + (left > 1); }
 template <typename T> __device__ __forceinline__ typename Pair<T>::Raw load_pair(const T *p, int count) {
     typename Pair<T>::Raw v = {};
     if (count == 2) v = *reinterpret_cast<const typename Pair<T>::Raw *>(p);
@@ -277,7 +281,7 @@ gated_scan_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     dependent_wait();
     const int strips = (p.features + kColumns - 1) / kColumns, item = blockIdx.x / ctas;
     const int sequence = item / strips, col0 = item % strips * kColumns, col = col0 + lane * 2;
-    const int count = max(0, min(2, p.features - col));
+    const int count = pair_count(p.features - col);
     // The state before the sequence is read ahead of the barriers: whoever writes the one after it, perhaps over the same memory
     // (out_last may be h0), does so behind them, whichever CTA of the cluster it is.
     const float *start = kBack ? p.d_last : p.h0;
@@ -452,7 +456,7 @@ gated_scan_short_kernel(const GatedScanArgs p)
     const int64_t pairs = (p.features + 1) / 2, item = (int64_t)blockIdx.x * kShortThreads + threadIdx.x;
     const int64_t sequence = item / pairs;
     if (sequence >= p.n_sequences) return;
-    const int col = (int)(item % pairs) * 2, count = min(2, p.features - col);
+    const int col = (int)(item % pairs) * 2, count = pair_count(p.features - col);
     const Span span(p, sequence);
     const int begin = span.begin, end = span.end;
     if (span.bad && col == 0) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
@@ -510,23 +514,23 @@ constexpr int kStepThreads = 128;
 
 template <typename T> struct Four {
     typename Pair<T>::Raw v[2];
-    __device__ __forceinline__ void ask(const T *p, int count) {
-        if (count == 4) {
+    __device__ __forceinline__ void ask(const T *p, int left) {
+        if (left >= 4) {
             if constexpr (sizeof(T) == 2) { const uint2 q = *reinterpret_cast<const uint2 *>(p); v[0] = q.x; v[1] = q.y; }
             else { const float4 q = *reinterpret_cast<const float4 *>(p); v[0] = make_float2(q.x, q.y); v[1] = make_float2(q.z, q.w); }
         } else {
-            v[0] = load_pair(p, min(count, 2));
-            v[1] = load_pair(p + 2, max(count - 2, 0));
+            v[0] = load_pair(p, pair_count(left));
+            v[1] = load_pair(p + 2, pair_count(left - 2));
         }
     }
 };
-template <typename T> __device__ __forceinline__ void store_four(T *p, int count, const float2 (&h)[2]) {
-    if (count == 4) {
+template <typename T> __device__ __forceinline__ void store_four(T *p, int left, const float2 (&h)[2]) {
+    if (left >= 4) {
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(packed<T>(h[0]), packed<T>(h[1]));
         else *reinterpret_cast<float4 *>(p) = make_float4(h[0].x, h[0].y, h[1].x, h[1].y);
     } else {
-        store_pair(p, min(count, 2), h[0]);
-        store_pair(p + 2, max(count - 2, 0), h[1]);
+        store_pair(p, pair_count(left), h[0]);
+        store_pair(p + 2, pair_count(left - 2), h[1]);
     }
 }
 
@@ -539,23 +543,23 @@ gated_scan_step_kernel(const GatedScanArgs p, unsigned fours)
     const unsigned at = (unsigned)(first - sequence0 * fours) + threadIdx.x, over = at / fours;
     const int64_t sequence = sequence0 + over;
     if (sequence >= p.n_sequences) return;
-    const int col = (int)(at - over * fours) * 4, count = min(4, p.features - col);
+    const int col = (int)(at - over * fours) * 4, left = p.features - col;
     Four<float> start;
-    if (p.h0) start.ask(p.h0 + sequence * p.ld_h0 + col, count);
+    if (p.h0) start.ask(p.h0 + sequence * p.ld_h0 + col, left);
     else start.v[0] = start.v[1] = both(0.f);
     const Span span(p, sequence);
     if (span.bad && col == 0) atomicOr(p.status, (unsigned)GS_DEV_BAD_VALUE);
     Four<T> x, gate;
     const auto ask = [&](int t) {
         if (t >= span.end) return;
-        x.ask((const T *)p.x + (int64_t)t * p.ld_x + col, count);
-        gate.ask((const T *)p.gate + (int64_t)t * p.ld_gate + col, count);
+        x.ask((const T *)p.x + (int64_t)t * p.ld_x + col, left);
+        gate.ask((const T *)p.gate + (int64_t)t * p.ld_gate + col, left);
     };
     ask(span.begin);
     const GateFactors factors;
     float2 h[2] = {start.v[0], start.v[1]};
     for (int t = span.begin; t < span.end; ++t) {
-        if (p.states && (t - span.begin) % kRows == 0) store_four(p.states + state_row(span.begin, sequence, t) * p.ld_states + col, count, h);
+        if (p.states && (t - span.begin) % kRows == 0) store_four(p.states + state_row(span.begin, sequence, t) * p.ld_states + col, left, h);
         typename Pair<T>::Raw rx[2] = {x.v[0], x.v[1]}, rg[2] = {gate.v[0], gate.v[1]};
         ask(t + 1);
         leave_out<T>(rg, rx);
@@ -565,9 +569,9 @@ gated_scan_step_kernel(const GatedScanArgs p, unsigned fours)
             gate_of(factors, gate_values<T>(rg[i]), a, c);
             h[i] = fma2(a, h[i], mul2(c, unpack<T>(rx[i])));
         }
-        if (p.out) store_four((T *)p.out + (int64_t)t * p.ld_out + col, count, h);
+        if (p.out) store_four((T *)p.out + (int64_t)t * p.ld_out + col, left, h);
     }
-    if (p.last) store_four(p.last + sequence * p.ld_last + col, count, h);
+    if (p.last) store_four(p.last + sequence * p.ld_last + col, left, h);
     dependent_end();
 }
 
