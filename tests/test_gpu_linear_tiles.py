@@ -16,6 +16,8 @@ from test_gpu_encoder import ACTS, BF16, F16, activation, clean_status, close, g
 SIZES = [
     (30011, 600, 130),       # 256 rows wide, 354 tiles: full and partial ones (88 of 256 features) in turn, four or five a pair
     (20000, 1160, 72),       # 256, 395 tiles: the last of five holds 136 features, so that a CTA of the pair has eight of them
+    (25003, 603, 72),        # 256, 294 tiles: the last piece of eight features holds three
+    (20005, 333, 40),        # 256, 158 tiles: 77 of 256 features, the last piece five
     (6200, 600, 264),        # 128, 147 tiles: two a pair; the last row tile has 56 rows
     (6150, 530, 40),         # 128, 147 tiles, the last row tile six rows: nothing for the warps of its second half
     (40, 40000, 64),         # 64, 157 tiles
