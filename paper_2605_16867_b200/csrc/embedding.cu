@@ -477,7 +477,11 @@ template <typename T> cudaError_t forward_as(gs_ctx *ctx, const EmbeddingArgs &a
 }
 
 // Sorted places of a group of lanes: many enough groups for short lists, few partial sums for long ones (524,288 tokens,
-// pieces of 64 / 128: 37 / 21 us to join them, 297 / 305 for the sums).
+// pieces of 64 / 128: 37 / 21 us to join them, 297 / 305 for the sums).  A whole gradient of 30,000 rows in a graph, pieces of
+// 16 / 32 / 64 / 128: 40,000 tokens 256 wide 48 / 54 / 60 / 67 us, 1024 wide 83 / 83 / 87 / 111; 66,000 tokens 55 / 61 / 75 / 91 and
+// 105 / 99 / 98 / 117; 262,144 tokens 143 / 118 / 107 / 138 and 246 / 212 / 202 / 196; 524,288 tokens 233 / 188 / 168 / 153 and
+// 427 / 361 / 325 / 318.  Rows of 32 values would have shorter pieces (66,000 tokens 47 / 57 / 72 / 88, 524,288 tokens 117 / 105 /
+// 109 / 137): the rule goes by the wide ones.
 int piece_of(int64_t n_tokens) { return n_tokens > 262144 ? 128 : n_tokens > 65536 ? 64 : 16; }
 
 int sort_ctas(const gs_ctx *, int64_t n) {
@@ -505,8 +509,11 @@ template <typename T> cudaError_t sum_as(gs_ctx *ctx, const EmbeddingArgs &a, Su
     return by_lanes(a.features, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         const unsigned sum_ctas = (unsigned)((p.n_pieces * L + kSumThreads - 1) / kSumThreads);
-        // (with few rows, several warps share 32 of them: 3,191 tokens of 6,422, 1455 wide: 60 us a call with one, 36)
-        p.zero_parts = a.vocabulary < 8192 ? 16 : a.vocabulary < 32768 ? 4 : 1;
+        // Where a table has few rows and most of them no token, four warps share 32 of them, each with its own bisections.  In a
+        // graph, one / four / sixteen: 3,191 tokens of 6,422 rows, 1455 wide, 58 / 37 / 37 us; 3,000 of 20,000, 1024 wide 48 / 39 /
+        // 44, 16 wide 29 / 27 / 35; with more tokens than rows, 100,000 of 20,000, 256 wide 72 / 78 / 86, of 6,000, 16 wide 60 /
+        // 58 / 67; with many rows, 3,000 of 100,000, 64 wide 31 / 39 / 54, 1024 wide 101 / 96 / 92.
+        p.zero_parts = a.vocabulary < 32768 && a.n_tokens < a.vocabulary ? 4 : 1;
         const int64_t rows = ((int64_t)a.vocabulary * p.zero_parts + 127) / 128, most = (int64_t)ctx->n_sm * 8;
         p.zero_ctas = (int)(rows < most ? rows : most);
         const unsigned slabs = (unsigned)((a.features + 8 * L - 1) / (8 * L));
