@@ -726,7 +726,8 @@ enum gs_activation {
  *               out [n_rows, out_features]; sums, bias, activation and residual are in float, each output rounded once
  *   bias        float [out_features] or NULL;   residual may be NULL, may be out itself
  *   out_z       z for the gradient of the activation, or NULL
- * n_rows 0 .. GS_MAX_EXPERT_ROWS.
+ * Sums of many terms of one sign come out too small by some 6e-9 of their value a term (the tensor cores cut off what a sum does not
+ * hold): less than the output's rounding up to 65,536 in_features in float16, 524,288 in bfloat16.  n_rows 0 .. GS_MAX_EXPERT_ROWS.
  */
 GS_API int gs_linear(gs_ctx *ctx, int dtype, const void *x, int64_t ld_x, int64_t n_rows, const void *w, int64_t ld_w,
                     const float *bias, int32_t in_features, int32_t out_features, int activation,

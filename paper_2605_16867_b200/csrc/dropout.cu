@@ -4,7 +4,9 @@
 // A lane takes eight columns, 16 bytes of 16-bit values: one turn of the generator gives 128 bits, sixteen for
 // each of them (p then has steps of 2^-16; with a whole word for every value the generator's instructions, twice as
 // many, would bound the kernel and not memory: they take 58 % of the issue slots as it is).  Bound by memory: 131,072 x 1024 in
-// 16 bits with a residual 134 us = 6.0 TB/s, 92 % of a plain copy's rate.
+// 16 bits with a residual 137 us = 5.9 TB/s, 90 % of a plain copy's rate (65,536 x 1024 in 32 bits 116 us = 6.9 TB/s).  Rows that are
+// not whole blocks of eight long take two turns a block, since the words of most blocks lie in two counters: the generator's
+// instructions bound them (131,072 x 1001 280 us, 65,536 x 1001 in 32 bits 142 us); rows with gaps between them take 169 us.
 #include "operators.cuh"
 #include "pairs.cuh"
 

@@ -145,6 +145,12 @@ struct RowsArgs {
     unsigned *status;
 };
 
+// (The sums of y and dx run over the whole contraction in one chain, in 32 bits in tensor memory, where the tensor cores cut off
+// what does not fit.  Over n terms of one sign they drift towards zero by 6e-9 n of their value: measured 1.2e-5 at 2048 terms, 2.5e-5 at
+// 4096, 1.0e-4 at 16,384, 3.9e-4 at 65,536, 6.1e-3 at 1,048,576.  The result is rounded to sixteen bits, half a step of which is
+// 4.9e-4 or 3.9e-3, so the chain is not broken up as those of dW are, whose results keep 32 bits: the distance of a layer of 65,536
+// rows, 2048 to 2048, with GELU from 64 bits is 1.7e-3 in norm, the rounding's own, as with products in 32 bits.)
+
 // ... of a dense layer (one expert, no offsets), with its epilogue:
 //   forward   first = z = sum + bias,   out = act(z) + add
 //   backward  first = v = sum + add,    out = act'(below) * v          (either output may be missing)

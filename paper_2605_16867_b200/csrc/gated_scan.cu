@@ -12,8 +12,9 @@
 // Bound by instruction issue as much as by memory: two columns share theirs (packed float instructions), and a
 // gate takes one exponential and one reciprocal for both of its factors; 21 instructions a value forwards in long sequences
 // (48 % of the issue slots), 29 forwards and 42 backwards where four warps share a sequence (71 and 62 %).  4 x 32,768 rows of 1024
-// in 16 bits: 187 us = 4.3 TB/s; 500 windows of up to 512 rows, 520 wide: 97 us forwards, 144 backwards (2.9 TB/s of what a step
-// cannot do without); 4,096 sequences of one row of 1024: 14 us.
+// in 16 bits: 188 us = 4.3 TB/s, backwards 322 us = 4.2 TB/s (half as wide in 32 bits 145 us = 5.6 TB/s and 211 us = 6.4 TB/s); 500
+// windows of up to 512 rows, 520 wide: 96 us forwards with the states kept and 146 backwards, 263 us a step, which is 3.1 TB/s of
+// the 803 MB that it cannot do without; 4,096 sequences of one row of 1024: 13.9 us = 4.2 TB/s (32 bits: 16.8 us = 5.0 TB/s).
 #include <type_traits>
 
 #include "operators.cuh"
@@ -109,8 +110,10 @@ template <typename T, int kCount> __device__ __forceinline__ void leave_out(cons
     }
 }
 
-// a = s(g) = 1 / (1 + e) and c = 1 - s(g) = e / (1 + e) with e = exp(-g), each to a few units of its last place.  The
-// exponent's rounding is made good to first order: of e alone, that makes both factors right.
+// a = s(g) = 1 / (1 + e) and c = 1 - s(g) = e / (1 + e) with e = exp(-g), each to a few units of its last place.  e is 2^t for
+// t = -g log2(e) rounded.  What t is off by is had exactly from a fused multiply-add (the error-free product of Ogita, Rump and Oishi
+// 2005), with what the factor itself lacks of log2(e) (a constant in two parts, as in Cody and Waite 1980), and is made good to first
+// order: 2^off = 1 + off ln 2.  Of e alone, that makes both factors right.
 // (The factors are held in registers: as constants each use of a pair would be two moves.)
 struct GateFactors {
     float2 log2_e = held(1.44269504f), minus = held(-1.44269504f), rest = held(-1.92596299e-8f), ln_2 = held(0.693147181f), one = held(1.f);
@@ -196,7 +199,7 @@ template <typename T, int kWarps_, bool kBack> struct Shape {
     static constexpr int kArrays = kBack ? 3 : 2;
     static constexpr uint32_t kStage = kArrays * kArray;
     static constexpr bool kWide = kWarps > 4;                                 // (the shape that clusters are made of)
-    static constexpr int kStages = kWide && kStage != 49152 ? 2 : 3;
+    static constexpr int kStages = kWide && !(kBack && sizeof(T) == 2) ? 2 : 3;      // (what fits beside the CTAs of an SM; wide and backwards, 32 bits take 96 KB a stage)
     static constexpr int kClusters = kWide ? kMaxCluster : 1;
     static constexpr int kCtasPerSm = kWide ? (kBack || sizeof(T) == 4 ? 1 : 2) : kBack ? 4 : 7;
     struct Exchange {
@@ -629,6 +632,8 @@ template <typename T, int kWarps, bool kBack> cudaError_t launch_tiles(gs_ctx *c
 //   sequence (500 windows of 256 rows on average, 520 wide: 97 us forwards and 144 backwards; with the wide shape 135 and 250);
 //   else the wide shape, with clusters along the sequence while the GPU has room for them (4 x 32,768 x 1024: clusters of two
 //   295 us, of four 187).
+// The lengths are known on the device alone: a long sequence among many short ones takes their shape (4,096 of one row and one of
+// 4,000, 1024 wide: 1.5 ms forwards and 6.5 backwards, where the long one by itself takes 15 and 28 us).
 template <typename T, bool kBack> cudaError_t scan_as(gs_ctx *ctx, const GatedScanArgs &a, cudaStream_t st) {
     constexpr int W = kWideWarps<T, kBack>;
     using S = Shape<T, W, kBack>;

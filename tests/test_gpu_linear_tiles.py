@@ -87,3 +87,20 @@ def test_gradient_of_the_rows(gs, rows, features, depth, name, dtype, around, bo
         gs.linear_backward(dz, x, w, dx=over if both else None, around=(over if both else a) if around else None, z_below=below, activation=name, dz_below=again)
         assert torch.equal(again, dz_below) and (not both or torch.equal(over, dx))
     assert gs.device_status() == 0
+
+
+@pytest.mark.parametrize("fan_in", [4096, 65536])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_long_sums_of_one_sign(gs, fan_in, dtype):  # noqa: F811
+    """The documented drift, 6e-9 of a sum's value a term (held here to 2^-27 a term), and the output's rounding; the order of the
+    terms inside an instruction is off by 2^-20 at most."""
+    g = gen(fan_in)
+    x = (torch.rand(500, fan_in, generator=g, device="cuda") + 0.5).to(dtype)
+    w = ((torch.rand(72, fan_in, generator=g, device="cuda") + 0.5) / fan_in).to(dtype)
+    out, dx = padded(500, 72, dtype), padded(500, 72, dtype)
+    gs.linear(x, w, out)
+    gs.linear_backward(x, padded(500, 72, dtype), w.T.contiguous(), dx=dx)
+    want = x.double() @ w.double().T
+    room = rounding(want, dtype) + (2.0 ** -27 * fan_in + 2.0 ** -20) * want
+    close(out, want, room)
+    close(dx, want, room)
